@@ -54,7 +54,8 @@ typedef enum buzz_status {
     BUZZ_EUNSUPPORTED = -5  /* valid request the kernels do not cover (shape, dtype) */
 } buzz_status;
 
-enum { BUZZ_FP32 = 0, BUZZ_FP16 = 1, BUZZ_BF16 = 2 };
+enum { BUZZ_FP32 = 0, BUZZ_FP16 = 1, BUZZ_BF16 = 2,
+       BUZZ_E4M3 = 3 /* rows of a paged cache only (buzz_paged_config_t.page_dtype) */ };
 
 enum {
     BUZZ_FLAG_AUTO_EVICT = 1u, /* buzz_decode_step evicts by itself when T new tokens are buffered */
@@ -284,6 +285,144 @@ typedef struct buzz_profile {
 } buzz_profile_t;
 int buzz_cache_profile(buzz_cache_t* cache, int enable);
 int buzz_cache_profile_read(buzz_cache_t* cache, buzz_profile_t* out);
+
+/*
+ * ---- What stands beside the bounded cache: position rotation, and a paged cache that keeps every token ----
+ *
+ * buzz_prefill and buzz_decode_step take queries and keys that are ready for the dot product, and one handle takes
+ * sequences of equal length.  buzz_qk_norm_rotate makes the former ready.  The paged cache holds sequences of any
+ * length, whole, until they are compressed (buzz_paged_read gives what buzz_prefill takes) or for as long as full
+ * attention is wanted (buzz_paged_decode).
+ *
+ * Rows.  A buzz_rows_t describes rows of head_dim elements [sequence][head][row], each row contiguous, the three
+ * distances in elements: slices of a projection's result can be given as they are.  `data` and the distances must be
+ * multiples of 16 bytes (BUZZ_EUNSUPPORTED otherwise; the distance of a dimension of one is not looked at).  Rows
+ * that are read may overlap each other; rows that are written may not, but may be the very rows that the same call
+ * reads.
+ *
+ * Ragged batches.  A call handles rows 0 .. n_rows - 1 of every sequence b, of which the first count[b] are there
+ * (NULL: all; values outside 0 .. n_rows are clamped); row t stands at position start[b] + t (NULL: 0 + t).  The
+ * others are neither read nor written, nor is anything of a sequence whose start is negative.  start and count are
+ * device arrays [batch].
+ */
+typedef struct buzz_rows {
+    void* data;
+    int64_t seq_stride, head_stride, row_stride;   /* elements */
+} buzz_rows_t;
+
+/*
+ * What is done to a query or key row x of position t before it is used, in 32 bits, rounded once at the end:
+ *   norm      x_i *= w_i / sqrt(mean(x^2) + eps), per head; q_weight / k_weight NULL: no norm of the queries / keys
+ *   rotation  pairs (i, i + rot_dim / 2), or with `interleaved` (2 i, 2 i + 1), i < rot_dim / 2, turn by the angle
+ *             t * inv_freq[i]; elements from rot_dim on stay.  The angle is formed in 64 bits, so that far positions
+ *             keep their phase.  rot_dim 0: none.
+ */
+typedef struct buzz_rotary {
+    const void* q_weight;      /* device [head_dim], the rows' dtype */
+    const void* k_weight;
+    const double* inv_freq;    /* device [rot_dim / 2], radians per position */
+    float eps;
+    int32_t rot_dim;           /* 0 .. head_dim, a multiple of 16 */
+    int32_t interleaved;
+    int32_t reserved;          /* must be 0 */
+} buzz_rotary_t;
+
+/*
+ * Norm and rotation of query and key rows, dense to dense: q [batch][n_q_heads][n_rows] to q_out, k likewise with
+ * n_kv_heads to k_out.  Either pair may be NULL (both of it).  dtype BUZZ_FP32 / FP16 / BF16, head_dim 64, 128 or 256.
+ * Errors: BUZZ_EINVAL, BUZZ_EUNSUPPORTED, BUZZ_EHIP.
+ */
+int buzz_qk_norm_rotate(int32_t dtype, int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const buzz_rotary_t* rotary,
+                        const buzz_rows_t* q, const buzz_rows_t* k, const buzz_rows_t* q_out, const buzz_rows_t* k_out,
+                        int32_t batch, int64_t n_rows, const int32_t* start, const int32_t* count, void* hip_stream);
+
+/*
+ * A paged cache: one layer's rows in a pool of pages that sequences own through a page table.  The pages belong to the
+ * caller, who may fill, read or copy them in this layout, g = the elements in 16 bytes (4, 8; 16 in 8 bits):
+ *   k       [n_pages][n_kv_heads][page_rows][head_dim]
+ *   v       [n_pages][n_kv_heads][page_rows / g][head_dim][g]     (g tokens of one column side by side: what a
+ *                                                                  matrix instruction takes as one operand)
+ *   k_exp   [n_pages][n_kv_heads][page_rows] uint8, v_exp likewise: 8-bit pages only, else NULL
+ * An 8-bit row holds e4m3 codes and one exponent e (1 .. 254): a value is code * 2^(e - 127).  Rows are written with
+ * the least e that brings their largest finite value to 448 or less, rounded to nearest even; the type has no
+ * infinity, so infinities become NaN like NaN itself.
+ *
+ * page_table is a device array [batch][table_cols] of page numbers: token j of sequence b is row j % page_rows of page
+ * page_table[b][j / page_rows].  Sequences may share pages that only are read.  Only the entries that a call needs are
+ * looked at.  A number outside 0 .. n_pages - 1 among them is never followed: what would have been written there is
+ * dropped, and what would have been computed from it (a sequence's output, the rows read) is NaN.
+ */
+typedef struct buzz_paged buzz_paged_t;
+
+typedef struct buzz_paged_config {
+    int32_t batch;         /* most sequences per call */
+    int32_t n_q_heads;     /* query heads; 1 to 8 times n_kv_heads */
+    int32_t n_kv_heads;
+    int32_t head_dim;      /* 64, 128 or 256 */
+    int32_t dtype;         /* of queries, of rows that come and go: BUZZ_FP32 / FP16 / BF16 */
+    int32_t page_dtype;    /* of the pages: dtype, or BUZZ_E4M3 where dtype has 16 bits */
+    int32_t page_rows;     /* tokens per page: 16, 32, 64, 128 or 256 */
+    int32_t n_pages;
+    int32_t table_cols;    /* page-table entries per sequence */
+    int32_t sink;          /* with window > 0 a new token attends to the last `window` tokens, itself included, and the */
+    int32_t window;        /* first `sink`; 0: to every token */
+    uint32_t flags;        /* BUZZ_FLAG_DRY_RUN: validation only */
+    float softmax_scale;   /* 0 => 1/sqrt(head_dim) */
+    int32_t reserved;      /* must be 0 */
+} buzz_paged_config_t;
+
+typedef struct buzz_pages {
+    void* k;               /* 16-byte aligned, all of them */
+    void* v;
+    uint8_t* k_exp;
+    uint8_t* v_exp;
+} buzz_pages_t;
+
+/* Bytes of device workspace of a paged cache (partial results of buzz_paged_decode).  Errors: BUZZ_EINVAL, BUZZ_EUNSUPPORTED. */
+int buzz_paged_workspace_bytes(const buzz_paged_config_t* cfg, size_t* bytes);
+
+/*
+ * Create a paged cache over the caller's pages and a workspace of at least buzz_paged_workspace_bytes() bytes, 256-byte
+ * aligned; both must outlive the handle.  Clears the workspace's counters on `hip_stream`: work on other streams has
+ * to wait for that.  Decode calls of one handle, and replays of graphs that hold such calls, must follow each other on
+ * one stream or be ordered by events: they share the workspace.  Several handles may stand over the same pages.
+ * Errors: as above, plus BUZZ_ECAPACITY (workspace too small), BUZZ_EHIP.
+ */
+int buzz_paged_create(const buzz_paged_config_t* cfg, const buzz_pages_t* pages, void* dev_workspace, size_t bytes,
+                      void* hip_stream, buzz_paged_t** out);
+
+/* Free the host handle.  NULL is allowed.  Errors: BUZZ_EINVAL on a stale handle. */
+int buzz_paged_destroy(buzz_paged_t* cache);
+
+/*
+ * Store rows: keys after norm and rotation (rotary NULL: as they are), values as they are; row t of sequence b becomes
+ * token start[b] + t.  Queries, where given (q and q_out, both or neither), go through the same pass to q_out.  Tokens
+ * beyond table_cols * page_rows are dropped.  No two rows of a call may go to the same row of a page.
+ * Errors: BUZZ_EINVAL, BUZZ_ECAPACITY (batch above the configuration's, n_rows above table_cols * page_rows),
+ *         BUZZ_EUNSUPPORTED (alignment), BUZZ_EHIP.
+ */
+int buzz_paged_append(buzz_paged_t* cache, const buzz_rotary_t* rotary, const buzz_rows_t* q, const buzz_rows_t* k,
+                      const buzz_rows_t* v, const buzz_rows_t* q_out, int32_t batch, int64_t n_rows,
+                      const int32_t* page_table, const int32_t* start, const int32_t* count, void* hip_stream);
+
+/*
+ * Rows back: tokens start[b] .. start[b] + count[b] - 1 to rows 0 .. of k and v (either may be NULL), in dtype.
+ * Tokens beyond table_cols * page_rows come back as NaN.  Errors as buzz_paged_append.
+ */
+int buzz_paged_read(buzz_paged_t* cache, const buzz_rows_t* k, const buzz_rows_t* v, int32_t batch, int64_t n_rows,
+                    const int32_t* page_table, const int32_t* start, const int32_t* count, void* hip_stream);
+
+/*
+ * Attention of one new token per sequence over its tokens 0 .. length[b] - 1 (device array; the new token's own row is
+ * among them once it is appended): out = softmax(scale * q . K^T) V and lse = log(sum(exp(scale * q . K^T))).
+ *   q     [batch][n_q_heads], rows of one query each (row_stride is not looked at)
+ *   out   [batch][n_q_heads][head_dim] fp32, contiguous, 16-byte aligned      lse  [batch][n_q_heads] fp32, or NULL
+ * A sequence without tokens gives zeros and -infinity; one whose length is negative or beyond table_cols * page_rows
+ * gives NaN.  Two calls with the same arguments give the same bits.
+ * Errors: BUZZ_EINVAL, BUZZ_ECAPACITY (batch), BUZZ_EUNSUPPORTED (alignment), BUZZ_EHIP.
+ */
+int buzz_paged_decode(buzz_paged_t* cache, const buzz_rows_t* q, int32_t batch, const int32_t* page_table,
+                      const int32_t* length, float* out, float* lse, void* hip_stream);
 
 /*
  * Benchmark aid: a plain 16-byte-per-thread device-to-device copy of `bytes` bytes (multiple of 16,

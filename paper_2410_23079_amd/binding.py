@@ -24,12 +24,15 @@ FLAG_INTERVAL_NEW = 128
 FLAG_DEVICE_MERGE = 256
 FLAG_GLOBAL_TOPK = 512
 DTYPE_CODES = {"fp32": 0, "fp16": 1, "bf16": 2}
+PAGE_DTYPE_CODES = dict(DTYPE_CODES, e4m3=3)
 
 EXPORTS = ["buzz_workspace_bytes", "buzz_cache_create", "buzz_prefill", "buzz_decode_step",
            "buzz_decode_step_static", "buzz_evict",
            "buzz_cache_destroy", "buzz_cache_len", "buzz_cache_export", "buzz_cache_import", "buzz_cache_set_splits",
            "buzz_cache_override_die_map", "buzz_cache_profile",
-           "buzz_cache_profile_read", "buzz_bench_copy", "buzz_suggest_threshold", "buzz_strerror"]
+           "buzz_cache_profile_read", "buzz_bench_copy", "buzz_suggest_threshold", "buzz_strerror",
+           "buzz_qk_norm_rotate", "buzz_paged_workspace_bytes", "buzz_paged_create", "buzz_paged_destroy",
+           "buzz_paged_append", "buzz_paged_read", "buzz_paged_decode"]
 
 
 class BuzzError(RuntimeError):
@@ -53,6 +56,27 @@ class _Profile(ctypes.Structure):
     _fields_ = [("attn_launches", ctypes.c_int64), ("epilogue_launches", ctypes.c_int64),
                 ("evictions", ctypes.c_int64), ("attn_ms", ctypes.c_double), ("epilogue_ms", ctypes.c_double),
                 ("evict_ms", ctypes.c_double), ("attn_row_bytes", ctypes.c_double)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class _PagedCfg(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "page_dtype",
+                                              "page_rows", "n_pages", "table_cols", "sink", "window")] + [
+        ("flags", ctypes.c_uint32), ("softmax_scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_exp", "v_exp")]
 
 
 @dataclass
@@ -113,6 +137,14 @@ def load_library():
     lib.buzz_bench_copy.argtypes = [P, P, ctypes.c_size_t, P]
     lib.buzz_suggest_threshold.argtypes = [ctypes.c_int32, ctypes.c_int32]
     lib.buzz_suggest_threshold.restype = ctypes.c_int64
+    R, I32 = ctypes.POINTER(_Rows), ctypes.c_int32
+    lib.buzz_qk_norm_rotate.argtypes = [I32, I32, I32, I32, ctypes.POINTER(_Rotary), R, R, R, R, I32, I64, P, P, P]
+    lib.buzz_paged_workspace_bytes.argtypes = [ctypes.POINTER(_PagedCfg), ctypes.POINTER(ctypes.c_size_t)]
+    lib.buzz_paged_create.argtypes = [ctypes.POINTER(_PagedCfg), ctypes.POINTER(_Pages), P, ctypes.c_size_t, P, ctypes.POINTER(P)]
+    lib.buzz_paged_destroy.argtypes = [P]
+    lib.buzz_paged_append.argtypes = [P, ctypes.POINTER(_Rotary), R, R, R, R, I32, I64, P, P, P, P]
+    lib.buzz_paged_read.argtypes = [P, R, R, I32, I64, P, P, P, P]
+    lib.buzz_paged_decode.argtypes = [P, R, I32, P, P, P, P, P]
     lib.buzz_strerror.argtypes = [ctypes.c_int]
     lib.buzz_strerror.restype = ctypes.c_char_p
     _lib = lib
@@ -249,3 +281,226 @@ class BuzzCache:
         _check(self._lib.buzz_cache_export(self._h, _ptr(K), _ptr(V), _ptr(score), _ptr(pos), self._stream(stream)),
                "buzz_cache_export")
         return K, V, score, pos
+
+
+# ---------------------------------------------------------------------------------------------- paged cache
+def _torch_dtypes():
+    import torch
+    return {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
+
+
+_dtypes = None
+
+
+def _dtype(name):
+    global _dtypes
+    if _dtypes is None:
+        _dtypes = _torch_dtypes()
+    return _dtypes[name]
+
+
+def _wrong(what, t, want):
+    raise BuzzError(-1, what, f"got {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}; {want}")
+
+
+def _rows(what, t, dtype, shape, device):
+    """Rows ``[batch, heads, n, D]`` (or ``[batch, heads, D]``) as the C ABI takes them; None stays None."""
+    if t is None:
+        return None
+    s = t.stride()
+    if t.dtype != dtype or t.shape != shape or s[-1] != 1 or t.device != device:
+        _wrong(what, t, f"wanted {tuple(shape)} {dtype} on {device} with contiguous rows")
+    return _Rows(t.data_ptr(), s[0], s[1], s[2] if len(s) == 4 else 0)
+
+
+def _ints(what, t, shape, device):
+    """Device pointer of a contiguous int32 tensor; None stays None."""
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != device:
+        _wrong(what, t, f"wanted {tuple(shape)} int32 on {device}, contiguous")
+    return t.data_ptr()
+
+
+def _gpu(what, device):
+    """Only tensors on the GPU are handed to kernels."""
+    if device.type != "cuda":
+        raise BuzzError(-1, what, f"tensors must be on the GPU, not on {device}")
+
+
+def _launch(device, stream, entry, *args):
+    """``entry(*args, stream)`` on the given stream or ``device``'s current one, with ``device`` current: kernels are
+    launched on the current device.  A dry-run cache (``device`` the CPU) launches nothing."""
+    if device.type != "cuda":
+        return entry(*args, None)
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(device).cuda_stream
+    elif type(stream) is not int:
+        stream = stream.cuda_stream
+    if torch.cuda.current_device() == device.index:
+        return entry(*args, stream)
+    with torch.cuda.device(device):
+        return entry(*args, stream)
+
+
+class Rotary:
+    """What is done to query and key rows before they are used: a norm per head (weights ``[head_dim]`` in the rows' dtype,
+    None: no norm) and the rotation of pairs by position * ``inv_freq`` (``[rot_dim / 2]`` float64, None: no rotation)."""
+
+    def __init__(self, q_weight=None, k_weight=None, inv_freq=None, eps: float = 1e-6, interleaved: bool = False):
+        import torch
+        for name, t in (("q_weight", q_weight), ("k_weight", k_weight), ("inv_freq", inv_freq)):
+            if t is not None and (t.dim() != 1 or not t.is_contiguous() or (t.dtype == torch.float64) != (name == "inv_freq")):
+                _wrong("Rotary " + name, t, "wanted a contiguous vector, inv_freq (and only it) in float64")
+        self.q_weight, self.k_weight, self.inv_freq = q_weight, k_weight, inv_freq        # kept alive
+        self.c = _Rotary(_ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), eps, 0 if inv_freq is None else 2 * inv_freq.numel(),
+                         int(interleaved), 0)
+
+    def check(self, dtype, head_dim, device):
+        for t in (self.q_weight, self.k_weight):
+            if t is not None and (t.dtype != dtype or t.numel() != head_dim or t.device != device):
+                _wrong("Rotary", t, f"wanted [{head_dim}] {dtype} on {device}")
+        if self.inv_freq is not None and self.inv_freq.device != device:
+            _wrong("Rotary inv_freq", self.inv_freq, f"wanted it on {device}")
+
+
+def qk_norm_rotate(q, k, q_out, k_out, rotary: Rotary, start=None, count=None, stream=None):
+    """Norm and rotation of query rows ``[batch, q heads, n, D]`` to ``q_out`` and key rows likewise to ``k_out`` (either
+    pair may be None, outputs may be the inputs).  Row t of sequence b stands at position ``start[b] + t``; ``count[b]`` rows
+    are there, the others stay as they were (int32 ``[batch]``; None: 0, all)."""
+    some = q if q is not None else k
+    if some is None:
+        raise BuzzError(-1, "qk_norm_rotate", "neither queries nor keys")
+    B, _, n, D = some.shape
+    dtype, device = some.dtype, some.device
+    _gpu("qk_norm_rotate", device)
+    code = {v: c for c, v in ((c, _dtype(name)) for name, c in DTYPE_CODES.items())}.get(dtype)
+    if code is None:
+        _wrong("qk_norm_rotate", some, "wanted fp32, fp16 or bf16")
+    rotary.check(dtype, D, device)
+    hq, hk = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
+    qs, ks = (B, hq, n, D), (B, hk, n, D)
+    _check(_launch(device, stream, load_library().buzz_qk_norm_rotate, code, D, hq, hk, rotary.c,
+                   _rows("qk_norm_rotate q", q, dtype, qs, device), _rows("qk_norm_rotate k", k, dtype, ks, device),
+                   _rows("qk_norm_rotate q_out", q_out, dtype, qs, device), _rows("qk_norm_rotate k_out", k_out, dtype, ks, device),
+                   B, n, _ints("qk_norm_rotate start", start, (B,), device), _ints("qk_norm_rotate count", count, (B,), device)),
+           "buzz_qk_norm_rotate")
+
+
+@dataclass
+class PagedConfig:
+    batch: int                     # most sequences per call
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    dtype: str                     # "fp32" | "fp16" | "bf16": rows that come and go
+    page_rows: int                 # tokens per page: 16, 32, 64, 128 or 256
+    n_pages: int
+    table_cols: int                # page-table entries per sequence
+    page_dtype: str | None = None  # None: dtype; "e4m3": 8 bits (16-bit dtype only)
+    sink: int = 0
+    window: int = 0                # 0: a new token attends to every token
+    softmax_scale: float = 0.0
+    flags: int = 0                 # FLAG_DRY_RUN
+
+    def to_c(self) -> _PagedCfg:
+        return _PagedCfg(self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim, DTYPE_CODES[self.dtype],
+                         PAGE_DTYPE_CODES[self.page_dtype or self.dtype], self.page_rows, self.n_pages, self.table_cols,
+                         self.sink, self.window, self.flags, self.softmax_scale, 0)
+
+
+def paged_workspace_bytes(cfg: PagedConfig) -> int:
+    out = ctypes.c_size_t()
+    _check(load_library().buzz_paged_workspace_bytes(cfg.to_c(), ctypes.byref(out)), "buzz_paged_workspace_bytes")
+    return out.value
+
+
+class PagedCache:
+    """One layer's paged cache.  ``pages`` = (k, v, k_exp, v_exp) stands over pages that exist already (the layout that
+    ``include/buzz.h`` gives); without it they are allocated, uninitialised, and kept as attributes of these names."""
+
+    def __init__(self, cfg: PagedConfig, device="cuda", pages=None, stream=None):
+        self.cfg = cfg
+        self._lib = load_library()
+        self._h = ctypes.c_void_p()
+        self.nbytes = paged_workspace_bytes(cfg)
+        self.dry = bool(cfg.flags & FLAG_DRY_RUN)
+        self.k_pages = self.v_pages = self.k_exp = self.v_exp = self.workspace = None
+        import torch
+        self.dtype, self.device = _dtype(cfg.dtype), torch.device("cpu")
+        raw, ws = _Pages(), None
+        if not self.dry:
+            e4m3 = cfg.page_dtype == "e4m3"
+            g = 16 // (1 if e4m3 else self.dtype.itemsize)
+            k_shape = (cfg.n_pages, cfg.n_kv_heads, cfg.page_rows, cfg.head_dim)
+            v_shape = (cfg.n_pages, cfg.n_kv_heads, cfg.page_rows // g, cfg.head_dim, g)
+            store = _dtype(cfg.page_dtype or cfg.dtype)
+            if pages is None:
+                exps = [torch.empty(k_shape[:3], dtype=torch.uint8, device=device) if e4m3 else None for _ in range(2)]
+                pages = (torch.empty(k_shape, dtype=store, device=device), torch.empty(v_shape, dtype=store, device=device), *exps)
+            self.device = pages[0].device
+            _gpu("PagedCache", self.device)
+            wanted = ((k_shape, store), (v_shape, store)) + (((k_shape[:3], torch.uint8),) * 2 if e4m3 else (None, None))
+            for t, want in zip(pages, wanted):
+                if (t is None) != (want is None):
+                    raise BuzzError(-1, "PagedCache", "exponents belong to 8-bit pages and only to them")
+                if t is not None and (t.shape != want[0] or t.dtype != want[1] or not t.is_contiguous() or t.device != self.device):
+                    _wrong("PagedCache pages", t, f"wanted {want[0]} {want[1]}, contiguous, all on one device")
+            self.k_pages, self.v_pages, self.k_exp, self.v_exp = pages
+            self.workspace = torch.empty(self.nbytes, dtype=torch.uint8, device=self.device)
+            raw, ws = _Pages(*map(_ptr, pages)), self.workspace.data_ptr()
+        c_cfg, entry = cfg.to_c(), self._lib.buzz_paged_create
+        _check(_launch(self.device, stream, lambda st: entry(c_cfg, raw, ws, self.nbytes, st, ctypes.byref(self._h))),
+               "buzz_paged_create")
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.buzz_paged_destroy(self._h)
+            self._h = None
+
+    __del__ = close
+
+    def append(self, k, v, table, start=None, count=None, q=None, q_out=None, rotary: Rotary | None = None, stream=None):
+        """Store rows ``[batch, kv heads, n, D]``: row t of sequence b becomes token ``start[b] + t``, keys after norm and
+        rotation.  Queries, if given, go through the same pass to ``q_out``.  ``table``: int32 ``[batch, table_cols]``."""
+        c = self.cfg
+        B, _, n, _ = k.shape
+        kv, qs = (B, c.n_kv_heads, n, c.head_dim), (B, c.n_q_heads, n, c.head_dim)
+        if rotary is not None:
+            rotary.check(self.dtype, c.head_dim, self.device)
+        _check(_launch(self.device, stream, self._lib.buzz_paged_append, self._h, None if rotary is None else rotary.c,
+                       _rows("append q", q, self.dtype, qs, self.device), _rows("append k", k, self.dtype, kv, self.device),
+                       _rows("append v", v, self.dtype, kv, self.device), _rows("append q_out", q_out, self.dtype, qs, self.device),
+                       B, n, _ints("append table", table, (B, c.table_cols), self.device),
+                       _ints("append start", start, (B,), self.device), _ints("append count", count, (B,), self.device)),
+               "buzz_paged_append")
+
+    def read(self, table, start, count, k, v, stream=None):
+        """Tokens ``start[b] ..`` of every sequence back into rows 0 .. ``count[b]`` - 1 of ``k`` and ``v``
+        ``[batch, kv heads, n, D]`` (either may be None)."""
+        c = self.cfg
+        some = k if k is not None else v
+        if some is None:
+            raise BuzzError(-1, "read", "neither keys nor values")
+        B, _, n, _ = some.shape
+        kv = (B, c.n_kv_heads, n, c.head_dim)
+        _check(_launch(self.device, stream, self._lib.buzz_paged_read, self._h, _rows("read k", k, self.dtype, kv, self.device),
+                       _rows("read v", v, self.dtype, kv, self.device), B, n,
+                       _ints("read table", table, (B, c.table_cols), self.device),
+                       _ints("read start", start, (B,), self.device), _ints("read count", count, (B,), self.device)),
+               "buzz_paged_read")
+
+    def decode(self, q, table, length, out, lse=None, stream=None):
+        """Attention of one new token per sequence, q ``[batch, q heads, D]``, over tokens 0 .. ``length[b]`` - 1; ``out``
+        fp32 like q, ``lse`` fp32 ``[batch, q heads]`` or None."""
+        import torch
+        c, B = self.cfg, q.shape[0]
+        for what, t, shape in (("decode out", out, (B, c.n_q_heads, c.head_dim)), ("decode lse", lse, (B, c.n_q_heads))):
+            if t is not None and (t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or t.device != self.device):
+                _wrong(what, t, f"wanted {shape} float32 on {self.device}, contiguous")
+        _check(_launch(self.device, stream, self._lib.buzz_paged_decode, self._h,
+                       _rows("decode q", q, self.dtype, (B, c.n_q_heads, c.head_dim), self.device), B,
+                       _ints("decode table", table, (B, c.table_cols), self.device), _ints("decode length", length, (B,), self.device),
+                       _ptr(out), _ptr(lse)), "buzz_paged_decode")

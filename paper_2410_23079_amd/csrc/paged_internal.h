@@ -1,0 +1,136 @@
+// Internal declarations of the paged cache and of the position rotation, shared by their host code and kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "buzz.h"
+
+namespace buzz {
+
+constexpr int kPagedMaxBlocks = 1024;      // blocks of a decode step; the workspace holds two partial results for each
+constexpr int kPagedTileTokens = 16;       // positions that one block of the row kernels works on: every page is whole tiles
+
+struct Rows {                              // [sequence][head][row][head_dim], distances in bytes
+    char* data;
+    int64_t seq, head, row;
+};
+
+// The pages of one cache.  `rows` is a power of two, so are the elements in 16 bytes (g): page rows of a lane's
+// 16-byte pieces never cross a page.
+struct PageArgs {
+    char* k; char* v;
+    uint8_t* k_exp; uint8_t* v_exp;        // NULL unless the pages hold 8 bits
+    const int32_t* table;                  // [batch][cols]
+    int32_t n_pages, rows, rows_log2, cols;
+    int32_t heads, D;
+};
+
+// The page of token j, or -1: a number that is none of the pool's is never followed.  The caller has made sure that
+// 0 <= j < cols * rows.
+__host__ __device__ inline int32_t page_of(const int32_t* table_row, int64_t j, int32_t rows_log2, int32_t n_pages)
+{
+    const int32_t p = table_row[j >> rows_log2];
+    return p >= 0 && p < n_pages ? p : -1;
+}
+
+// Which rows of a sequence a call handles: positions [lo, hi) of rows lo - start ..; empty where nothing is there.
+struct Span { int64_t start, lo, hi; };
+__host__ __device__ inline Span row_span(const int32_t* start, const int32_t* count, int b, int64_t n_rows)
+{
+    const int64_t s = start ? start[b] : 0;
+    int64_t n = count ? count[b] : n_rows;
+    n = n < 0 ? 0 : n > n_rows ? n_rows : n;
+    return s < 0 ? Span{0, 0, 0} : Span{s, s, s + n};
+}
+
+// Tiles of 16 positions that n rows can touch, wherever the first one stands.
+__host__ __device__ inline int64_t tiles_of_rows(int64_t n) { return n <= 0 ? 0 : (n + 14) / kPagedTileTokens + 1; }
+
+// Keys that the new token of a sequence of `length` tokens attends to: [0, sink_end) and [from, length).
+struct Visible {
+    int32_t length, from, sink_end;        // length < 0: the caller's length is none
+    __host__ __device__ inline bool sees(int32_t j) const { return j < length && (j >= from || j < sink_end); }
+};
+__host__ __device__ inline Visible visible(int32_t length, int32_t sink, int32_t window, int64_t most)
+{
+    if (length < 0 || length > most) return Visible{-1, 0, 0};
+    const int32_t from = window > 0 && length > window ? length - window : 0;
+    return Visible{length, from, sink < from ? sink : from};
+}
+
+// The tiles of `tile` keys that hold them, in order: the first `low` ones, then those from `high` on; `count` in all.
+struct Tiles {
+    int32_t low, high, count;
+    __host__ __device__ inline int32_t at(int32_t i) const { return i < low ? i : high + (i - low); }
+};
+__host__ __device__ inline Tiles tiles_of(const Visible& v, int32_t tile)
+{
+    if (v.length <= 0) return Tiles{0, 0, 0};
+    const int32_t end = (v.length - 1) / tile + 1, high = v.from / tile;
+    int32_t low = v.sink_end > 0 ? (v.sink_end - 1) / tile + 1 : 0;
+    if (low > high) low = high;
+    return Tiles{low, high, low + end - high};
+}
+
+// A decode step's tiles, numbered through over all (sequence, head) pairs, `share` consecutive ones to a block, four at
+// least (one per wave).  A pair of n tiles from number `begin` on is worked on by `parts` blocks from `from` on; each but the
+// one with the pair's first tile leaves its partial result in its slot 0, that one in slot 1, so a block that ends one pair
+// and begins another needs two.
+__host__ __device__ inline uint64_t tiles_per_block(uint64_t total, unsigned blocks)
+{
+    const uint64_t share = (total + blocks - 1) / blocks;
+    return share < 4 ? 4 : share;
+}
+struct Parts {
+    int from, parts;
+    __host__ __device__ inline int64_t slot(int i) const { return 2 * (int64_t)(from + i) + (i == 0 ? 1 : 0); }
+};
+__host__ __device__ inline Parts parts_of(uint64_t begin, uint64_t n, uint64_t share)
+{
+    const int from = (int)(begin / share);
+    return Parts{from, (int)((begin + n - 1) / share) - from + 1};
+}
+
+struct RotateArgs {
+    Rows q, k, v, q_out, k_out;            // data NULL: not there; k_out of the dense form only
+    const void* q_weight; const void* k_weight;
+    const double* inv_freq;
+    const int32_t* start; const int32_t* count;
+    int64_t n_rows;
+    float eps;
+    int32_t half;                          // rot_dim / 2
+    int32_t interleaved;
+    int32_t Hq, Hkv, D;
+    int32_t q_chunk, kv_chunk, q_jobs, k_jobs, v_jobs;   // heads per block; blocks (grid's y) per tile of positions (set by the launch)
+    PageArgs pages;                        // k NULL: dense
+};
+
+struct ReadArgs {
+    Rows k, v;
+    const int32_t* start; const int32_t* count;
+    int64_t n_rows;
+    PageArgs pages;
+    int32_t chunk, k_jobs, v_jobs;         // set by the launch
+};
+
+struct PagedAttnArgs {
+    const char* q;
+    int64_t q_seq, q_head;                 // bytes
+    float* out; float* lse;
+    const int32_t* length;
+    PageArgs pages;
+    float* part_o;                         // [blocks][2][G][D] unnormalised outputs
+    float* part_ml;                        // [blocks][2][G][2] (reference, sum)
+    int32_t* ticket;                       // [batch * heads], zero between launches
+    int32_t batch, G;
+    int32_t sink, window;
+    float scale_log2;
+};
+
+hipError_t launch_rotate(int dtype, int page_dtype, const RotateArgs& a, int batch, hipStream_t st);
+hipError_t launch_paged_read(int dtype, int page_dtype, const ReadArgs& a, int batch, hipStream_t st);
+hipError_t launch_paged_attn(int dtype, int page_dtype, const PagedAttnArgs& a, int compute_units, hipStream_t st);
+hipError_t launch_clear_f32(float* dst, int64_t n, hipStream_t st);
+
+}  // namespace buzz
