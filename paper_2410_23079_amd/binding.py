@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -56,11 +57,6 @@ class _Profile(ctypes.Structure):
     _fields_ = [("attn_launches", ctypes.c_int64), ("epilogue_launches", ctypes.c_int64),
                 ("evictions", ctypes.c_int64), ("attn_ms", ctypes.c_double), ("epilogue_ms", ctypes.c_double),
                 ("evict_ms", ctypes.c_double), ("attn_row_bytes", ctypes.c_double)]
-
-
-class _Rows(ctypes.Structure):
-    _fields_ = [("data", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
-                ("row_stride", ctypes.c_int64)]
 
 
 class _Rotary(ctypes.Structure):
@@ -137,14 +133,14 @@ def load_library():
     lib.buzz_bench_copy.argtypes = [P, P, ctypes.c_size_t, P]
     lib.buzz_suggest_threshold.argtypes = [ctypes.c_int32, ctypes.c_int32]
     lib.buzz_suggest_threshold.restype = ctypes.c_int64
-    R, I32 = ctypes.POINTER(_Rows), ctypes.c_int32
-    lib.buzz_qk_norm_rotate.argtypes = [I32, I32, I32, I32, ctypes.POINTER(_Rotary), R, R, R, R, I32, I64, P, P, P]
+    I32 = ctypes.c_int32
+    lib.buzz_qk_norm_rotate.argtypes = [I32, I32, I32, I32, P, P, P, P, P, I32, I64, P, P, P]
     lib.buzz_paged_workspace_bytes.argtypes = [ctypes.POINTER(_PagedCfg), ctypes.POINTER(ctypes.c_size_t)]
     lib.buzz_paged_create.argtypes = [ctypes.POINTER(_PagedCfg), ctypes.POINTER(_Pages), P, ctypes.c_size_t, P, ctypes.POINTER(P)]
     lib.buzz_paged_destroy.argtypes = [P]
-    lib.buzz_paged_append.argtypes = [P, ctypes.POINTER(_Rotary), R, R, R, R, I32, I64, P, P, P, P]
-    lib.buzz_paged_read.argtypes = [P, R, R, I32, I64, P, P, P, P]
-    lib.buzz_paged_decode.argtypes = [P, R, I32, P, P, P, P, P]
+    lib.buzz_paged_append.argtypes = [P, P, P, P, P, P, I32, I64, P, P, P, P]
+    lib.buzz_paged_read.argtypes = [P, P, P, I32, I64, P, P, P, P]
+    lib.buzz_paged_decode.argtypes = [P, P, I32, P, P, P, P, P]
     lib.buzz_strerror.argtypes = [ctypes.c_int]
     lib.buzz_strerror.restype = ctypes.c_char_p
     _lib = lib
@@ -284,18 +280,16 @@ class BuzzCache:
 
 
 # ---------------------------------------------------------------------------------------------- paged cache
-def _torch_dtypes():
-    import torch
-    return {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn}
-
-
-_dtypes = None
+# A decode step takes the GPU some 5 us, and the host has to keep up: rows go to the C ABI as packed bytes (a ctypes structure
+# takes three times as long to make), and tensors are looked at by their cheapest attributes.
+_pack_rows = struct.Struct("Pqqq").pack                    # buzz_rows_t
+_dtypes = {}
 
 
 def _dtype(name):
-    global _dtypes
-    if _dtypes is None:
-        _dtypes = _torch_dtypes()
+    if not _dtypes:
+        import torch
+        _dtypes.update(fp32=torch.float32, fp16=torch.float16, bf16=torch.bfloat16, e4m3=torch.float8_e4m3fn, int32=torch.int32)
     return _dtypes[name]
 
 
@@ -303,23 +297,22 @@ def _wrong(what, t, want):
     raise BuzzError(-1, what, f"got {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}; {want}")
 
 
-def _rows(what, t, dtype, shape, device):
-    """Rows ``[batch, heads, n, D]`` (or ``[batch, heads, D]``) as the C ABI takes them; None stays None."""
+def _rows(what, t, dtype, shape, index):
+    """Rows ``[batch, heads, n, D]`` or ``[batch, heads, D]`` of GPU ``index`` (-1: the CPU) as the C ABI takes them; None stays None."""
     if t is None:
         return None
     s = t.stride()
-    if t.dtype != dtype or t.shape != shape or s[-1] != 1 or t.device != device:
-        _wrong(what, t, f"wanted {tuple(shape)} {dtype} on {device} with contiguous rows")
-    return _Rows(t.data_ptr(), s[0], s[1], s[2] if len(s) == 4 else 0)
+    if t.dtype is not dtype or t.shape != shape or s[-1] != 1 or t.get_device() != index:
+        _wrong(what, t, f"wanted {tuple(shape)} {dtype} on device {index} with contiguous rows")
+    return _pack_rows(t.data_ptr(), s[0], s[1], s[2])
 
 
-def _ints(what, t, shape, device):
-    """Device pointer of a contiguous int32 tensor; None stays None."""
+def _dense(what, t, dtype, shape, index):
+    """Device pointer of a contiguous tensor; None stays None."""
     if t is None:
         return None
-    import torch
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != device:
-        _wrong(what, t, f"wanted {tuple(shape)} int32 on {device}, contiguous")
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != index:
+        _wrong(what, t, f"wanted {tuple(shape)} {dtype} on device {index}, contiguous")
     return t.data_ptr()
 
 
@@ -329,19 +322,23 @@ def _gpu(what, device):
         raise BuzzError(-1, what, f"tensors must be on the GPU, not on {device}")
 
 
-def _launch(device, stream, entry, *args):
-    """``entry(*args, stream)`` on the given stream or ``device``'s current one, with ``device`` current: kernels are
-    launched on the current device.  A dry-run cache (``device`` the CPU) launches nothing."""
-    if device.type != "cuda":
+_gpus = 0
+
+
+def _launch(index, stream, entry, *args):
+    """``entry(*args, stream)`` on the given stream or the current one of GPU ``index``, with that GPU current: kernels are
+    launched on the current device.  A dry-run cache (-1) launches nothing."""
+    global _gpus
+    if index < 0:
         return entry(*args, None)
-    import torch
-    if stream is None:
-        stream = torch.cuda.current_stream(device).cuda_stream
-    elif type(stream) is not int:
-        stream = stream.cuda_stream
-    if torch.cuda.current_device() == device.index:
+    if type(stream) is not int:
+        import torch
+        stream = torch.cuda.current_stream(index).cuda_stream if stream is None else stream.cuda_stream
+    if _gpus == 1:
         return entry(*args, stream)
-    with torch.cuda.device(device):
+    import torch
+    _gpus = torch.cuda.device_count()
+    with torch.cuda.device(index):
         return entry(*args, stream)
 
 
@@ -357,13 +354,15 @@ class Rotary:
         self.q_weight, self.k_weight, self.inv_freq = q_weight, k_weight, inv_freq        # kept alive
         self.c = _Rotary(_ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), eps, 0 if inv_freq is None else 2 * inv_freq.numel(),
                          int(interleaved), 0)
+        self.ref = ctypes.addressof(self.c)
 
-    def check(self, dtype, head_dim, device):
+    def check(self, dtype, head_dim, index):
         for t in (self.q_weight, self.k_weight):
-            if t is not None and (t.dtype != dtype or t.numel() != head_dim or t.device != device):
-                _wrong("Rotary", t, f"wanted [{head_dim}] {dtype} on {device}")
-        if self.inv_freq is not None and self.inv_freq.device != device:
-            _wrong("Rotary inv_freq", self.inv_freq, f"wanted it on {device}")
+            if t is not None and (t.dtype is not dtype or t.shape[0] != head_dim or t.get_device() != index):
+                _wrong("Rotary", t, f"wanted [{head_dim}] {dtype} on device {index}")
+        if self.inv_freq is not None and self.inv_freq.get_device() != index:
+            _wrong("Rotary inv_freq", self.inv_freq, f"wanted it on device {index}")
+        return self.ref
 
 
 def qk_norm_rotate(q, k, q_out, k_out, rotary: Rotary, start=None, count=None, stream=None):
@@ -374,19 +373,20 @@ def qk_norm_rotate(q, k, q_out, k_out, rotary: Rotary, start=None, count=None, s
     if some is None:
         raise BuzzError(-1, "qk_norm_rotate", "neither queries nor keys")
     B, _, n, D = some.shape
-    dtype, device = some.dtype, some.device
-    _gpu("qk_norm_rotate", device)
-    code = {v: c for c, v in ((c, _dtype(name)) for name, c in DTYPE_CODES.items())}.get(dtype)
-    if code is None:
+    dtype, at, i32 = some.dtype, some.get_device(), _dtype("int32")
+    if at < 0:
+        _gpu("qk_norm_rotate", some.device)
+    code = 2 if dtype is _dtypes["bf16"] else 1 if dtype is _dtypes["fp16"] else 0 if dtype is _dtypes["fp32"] else -1
+    if code < 0:
         _wrong("qk_norm_rotate", some, "wanted fp32, fp16 or bf16")
-    rotary.check(dtype, D, device)
     hq, hk = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
     qs, ks = (B, hq, n, D), (B, hk, n, D)
-    _check(_launch(device, stream, load_library().buzz_qk_norm_rotate, code, D, hq, hk, rotary.c,
-                   _rows("qk_norm_rotate q", q, dtype, qs, device), _rows("qk_norm_rotate k", k, dtype, ks, device),
-                   _rows("qk_norm_rotate q_out", q_out, dtype, qs, device), _rows("qk_norm_rotate k_out", k_out, dtype, ks, device),
-                   B, n, _ints("qk_norm_rotate start", start, (B,), device), _ints("qk_norm_rotate count", count, (B,), device)),
-           "buzz_qk_norm_rotate")
+    rc = _launch(at, stream, load_library().buzz_qk_norm_rotate, code, D, hq, hk, rotary.check(dtype, D, at),
+                 _rows("qk_norm_rotate q", q, dtype, qs, at), _rows("qk_norm_rotate k", k, dtype, ks, at),
+                 _rows("qk_norm_rotate q_out", q_out, dtype, qs, at), _rows("qk_norm_rotate k_out", k_out, dtype, ks, at),
+                 B, n, _dense("qk_norm_rotate start", start, i32, (B,), at), _dense("qk_norm_rotate count", count, i32, (B,), at))
+    if rc:
+        _check(rc, "buzz_qk_norm_rotate")
 
 
 @dataclass
@@ -429,7 +429,7 @@ class PagedCache:
         self.dry = bool(cfg.flags & FLAG_DRY_RUN)
         self.k_pages = self.v_pages = self.k_exp = self.v_exp = self.workspace = None
         import torch
-        self.dtype, self.device = _dtype(cfg.dtype), torch.device("cpu")
+        self.dtype, self.at = _dtype(cfg.dtype), -1        # the GPU's number; -1: none
         raw, ws = _Pages(), None
         if not self.dry:
             e4m3 = cfg.page_dtype == "e4m3"
@@ -440,20 +440,23 @@ class PagedCache:
             if pages is None:
                 exps = [torch.empty(k_shape[:3], dtype=torch.uint8, device=device) if e4m3 else None for _ in range(2)]
                 pages = (torch.empty(k_shape, dtype=store, device=device), torch.empty(v_shape, dtype=store, device=device), *exps)
-            self.device = pages[0].device
-            _gpu("PagedCache", self.device)
-            wanted = ((k_shape, store), (v_shape, store)) + (((k_shape[:3], torch.uint8),) * 2 if e4m3 else (None, None))
-            for t, want in zip(pages, wanted):
-                if (t is None) != (want is None):
-                    raise BuzzError(-1, "PagedCache", "exponents belong to 8-bit pages and only to them")
-                if t is not None and (t.shape != want[0] or t.dtype != want[1] or not t.is_contiguous() or t.device != self.device):
-                    _wrong("PagedCache pages", t, f"wanted {want[0]} {want[1]}, contiguous, all on one device")
+            _gpu("PagedCache", pages[0].device)
+            self.at = pages[0].get_device()
+            exps = ("PagedCache exponents", torch.uint8, k_shape[:3])
+            wanted = (("PagedCache k", store, k_shape), ("PagedCache v", store, v_shape)) + ((exps, exps) if e4m3 else (None, None))
+            if any((t is None) != (want is None) for t, want in zip(pages, wanted)):
+                raise BuzzError(-1, "PagedCache", "exponents belong to 8-bit pages and only to them")
+            raw = _Pages(*(None if t is None else _dense(want[0], t, want[1], want[2], self.at) for t, want in zip(pages, wanted)))
             self.k_pages, self.v_pages, self.k_exp, self.v_exp = pages
-            self.workspace = torch.empty(self.nbytes, dtype=torch.uint8, device=self.device)
-            raw, ws = _Pages(*map(_ptr, pages)), self.workspace.data_ptr()
+            self.workspace = torch.empty(self.nbytes, dtype=torch.uint8, device=pages[0].device)
+            ws = self.workspace.data_ptr()
         c_cfg, entry = cfg.to_c(), self._lib.buzz_paged_create
-        _check(_launch(self.device, stream, lambda st: entry(c_cfg, raw, ws, self.nbytes, st, ctypes.byref(self._h))),
+        _check(_launch(self.at, stream, lambda st: entry(c_cfg, raw, ws, self.nbytes, st, ctypes.byref(self._h))),
                "buzz_paged_create")
+        # what every call compares its tensors with
+        self._table = cfg.table_cols
+        self._heads = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
+        self._f32, self._i32 = _dtype("fp32"), _dtype("int32")
 
     def close(self):
         if getattr(self, "_h", None):
@@ -465,42 +468,39 @@ class PagedCache:
     def append(self, k, v, table, start=None, count=None, q=None, q_out=None, rotary: Rotary | None = None, stream=None):
         """Store rows ``[batch, kv heads, n, D]``: row t of sequence b becomes token ``start[b] + t``, keys after norm and
         rotation.  Queries, if given, go through the same pass to ``q_out``.  ``table``: int32 ``[batch, table_cols]``."""
-        c = self.cfg
+        hq, h, D = self._heads
         B, _, n, _ = k.shape
-        kv, qs = (B, c.n_kv_heads, n, c.head_dim), (B, c.n_q_heads, n, c.head_dim)
-        if rotary is not None:
-            rotary.check(self.dtype, c.head_dim, self.device)
-        _check(_launch(self.device, stream, self._lib.buzz_paged_append, self._h, None if rotary is None else rotary.c,
-                       _rows("append q", q, self.dtype, qs, self.device), _rows("append k", k, self.dtype, kv, self.device),
-                       _rows("append v", v, self.dtype, kv, self.device), _rows("append q_out", q_out, self.dtype, qs, self.device),
-                       B, n, _ints("append table", table, (B, c.table_cols), self.device),
-                       _ints("append start", start, (B,), self.device), _ints("append count", count, (B,), self.device)),
-               "buzz_paged_append")
+        dt, at, i32, kv, qs = self.dtype, self.at, self._i32, (B, h, n, D), (B, hq, n, D)
+        rc = _launch(at, stream, self._lib.buzz_paged_append, self._h, None if rotary is None else rotary.check(dt, D, at),
+                     _rows("append q", q, dt, qs, at), _rows("append k", k, dt, kv, at), _rows("append v", v, dt, kv, at),
+                     _rows("append q_out", q_out, dt, qs, at), B, n, _dense("append table", table, i32, (B, self._table), at),
+                     _dense("append start", start, i32, (B,), at), _dense("append count", count, i32, (B,), at))
+        if rc:
+            _check(rc, "buzz_paged_append")
 
     def read(self, table, start, count, k, v, stream=None):
         """Tokens ``start[b] ..`` of every sequence back into rows 0 .. ``count[b]`` - 1 of ``k`` and ``v``
         ``[batch, kv heads, n, D]`` (either may be None)."""
-        c = self.cfg
         some = k if k is not None else v
         if some is None:
             raise BuzzError(-1, "read", "neither keys nor values")
+        _, h, D = self._heads
         B, _, n, _ = some.shape
-        kv = (B, c.n_kv_heads, n, c.head_dim)
-        _check(_launch(self.device, stream, self._lib.buzz_paged_read, self._h, _rows("read k", k, self.dtype, kv, self.device),
-                       _rows("read v", v, self.dtype, kv, self.device), B, n,
-                       _ints("read table", table, (B, c.table_cols), self.device),
-                       _ints("read start", start, (B,), self.device), _ints("read count", count, (B,), self.device)),
-               "buzz_paged_read")
+        dt, at, i32, kv = self.dtype, self.at, self._i32, (B, h, n, D)
+        rc = _launch(at, stream, self._lib.buzz_paged_read, self._h, _rows("read k", k, dt, kv, at), _rows("read v", v, dt, kv, at),
+                     B, n, _dense("read table", table, i32, (B, self._table), at), _dense("read start", start, i32, (B,), at),
+                     _dense("read count", count, i32, (B,), at))
+        if rc:
+            _check(rc, "buzz_paged_read")
 
     def decode(self, q, table, length, out, lse=None, stream=None):
         """Attention of one new token per sequence, q ``[batch, q heads, D]``, over tokens 0 .. ``length[b]`` - 1; ``out``
         fp32 like q, ``lse`` fp32 ``[batch, q heads]`` or None."""
-        import torch
-        c, B = self.cfg, q.shape[0]
-        for what, t, shape in (("decode out", out, (B, c.n_q_heads, c.head_dim)), ("decode lse", lse, (B, c.n_q_heads))):
-            if t is not None and (t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or t.device != self.device):
-                _wrong(what, t, f"wanted {shape} float32 on {self.device}, contiguous")
-        _check(_launch(self.device, stream, self._lib.buzz_paged_decode, self._h,
-                       _rows("decode q", q, self.dtype, (B, c.n_q_heads, c.head_dim), self.device), B,
-                       _ints("decode table", table, (B, c.table_cols), self.device), _ints("decode length", length, (B,), self.device),
-                       _ptr(out), _ptr(lse)), "buzz_paged_decode")
+        hq, _, D = self._heads
+        at, i32, B = self.at, self._i32, q.shape[0]
+        shape = (B, hq, D)
+        rc = _launch(at, stream, self._lib.buzz_paged_decode, self._h, _rows("decode q", q, self.dtype, shape, at), B,
+                     _dense("decode table", table, i32, (B, self._table), at), _dense("decode length", length, i32, (B,), at),
+                     _dense("decode out", out, self._f32, shape, at), _dense("decode lse", lse, self._f32, shape[:2], at))
+        if rc:
+            _check(rc, "buzz_paged_decode")

@@ -17,7 +17,7 @@ SOURCES = [("buzz_api.cpp", "buzz_api", []), ("evict_kernels.hip", "evict_kernel
            ("attn_kernels.hip", "attn_fp32", ["-DBUZZ_TU=0"]), ("attn_kernels.hip", "attn_fp16", ["-DBUZZ_TU=1"]),
            ("attn_kernels.hip", "attn_bf16", ["-DBUZZ_TU=2"]), ("attn_kernels.hip", "attn_common", ["-DBUZZ_TU=3"]),
            ("paged_api.cpp", "paged_api", []), ("paged_row_kernels.hip", "paged_row_kernels", []),
-           ("paged_attn_kernels.hip", "paged_attn_kernels", [])]
+           ("paged_attn_kernels.hip", "paged_attn_kernels", ["-mllvm", "-amdgpu-mfma-vgpr-form"])]
 FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc",
     # packed fp32 VALU forms are switched off for the whole library

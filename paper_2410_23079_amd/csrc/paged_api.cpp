@@ -19,7 +19,7 @@ int elem_bytes(int dtype) { return dtype == BUZZ_FP32 ? 4 : 2; }
 bool head_dim_ok(int d) { return d == 64 || d == 128 || d == 256; }
 int hip_rc(hipError_t e) { return e == hipSuccess ? BUZZ_OK : BUZZ_EHIP; }
 
-struct PagedLayout { size_t ticket, part_ml, part_o, total; };
+struct PagedLayout { size_t ticket, group_ticket, counters, part_ml, part_o, total; };
 
 int make_layout(const buzz_paged_config_t* c, PagedLayout* L)
 {
@@ -32,9 +32,13 @@ int make_layout(const buzz_paged_config_t* c, PagedLayout* L)
     if (!head_dim_ok(c->head_dim) || G > 8 || (c->page_dtype == BUZZ_E4M3 && c->dtype == BUZZ_FP32)) return BUZZ_EUNSUPPORTED;
     if (!is_power(c->page_rows) || c->page_rows < kPagedTileTokens || c->page_rows > 256) return BUZZ_EUNSUPPORTED;
     if (c->batch > 65535 || c->n_kv_heads > 65535 || (int64_t)c->table_cols * c->page_rows > kMaxTokens) return BUZZ_EUNSUPPORTED;
+    if ((double)c->n_kv_heads * c->page_rows * c->head_dim * elem_bytes(c->dtype) >= 4294967296.0) return BUZZ_EUNSUPPORTED;
+    if (!units_countable(c->batch, c->n_kv_heads, c->table_cols, c->page_rows)) return BUZZ_EUNSUPPORTED;
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off += align_up(bytes); return at; };
     L->ticket = take((size_t)c->batch * c->n_kv_heads * sizeof(int32_t));
+    L->group_ticket = take((size_t)2 * kPagedMaxBlocks * sizeof(int32_t));
+    L->counters = off / sizeof(int32_t);               // all of them from the start of the workspace
     L->part_ml = take((size_t)2 * kPagedMaxBlocks * G * 2 * sizeof(float));
     L->part_o = take((size_t)2 * kPagedMaxBlocks * G * c->head_dim * sizeof(float));
     L->total = off;
@@ -172,7 +176,7 @@ int buzz_paged_create(const buzz_paged_config_t* cfg, const buzz_pages_t* pages,
     c->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / sqrtf((float)cfg->head_dim);
     c->dry = dry;
     if (!dry) {
-        if (hipError_t e = launch_clear_f32((float*)(c->ws + L.ticket), (int64_t)cfg->batch * cfg->n_kv_heads, (hipStream_t)hip_stream)) {
+        if (hipError_t e = launch_clear_f32((float*)c->ws, (int64_t)L.counters, (hipStream_t)hip_stream)) {
             delete c;
             return hip_rc(e);
         }
@@ -246,11 +250,13 @@ int buzz_paged_decode(buzz_paged_t* c, const buzz_rows_t* q, int32_t batch, cons
     a.length = length;
     a.pages = c->args(page_table);
     a.ticket = (int32_t*)(c->ws + c->L.ticket);
+    a.group_ticket = (int32_t*)(c->ws + c->L.group_ticket);
     a.part_ml = (float*)(c->ws + c->L.part_ml);
     a.part_o = (float*)(c->ws + c->L.part_o);
     a.batch = batch; a.G = cfg.n_q_heads / cfg.n_kv_heads;
     a.sink = cfg.sink; a.window = cfg.window;
     a.scale_log2 = c->scale * 1.4426950408889634f;
+    a.page_bytes = (uint32_t)cfg.n_kv_heads * cfg.page_rows * cfg.head_dim * (cfg.page_dtype == BUZZ_E4M3 ? 1 : elem_bytes(cfg.dtype));
     return hip_rc(launch_paged_attn(cfg.dtype, cfg.page_dtype, a, compute_units(), (hipStream_t)hip_stream));
 }
 

@@ -37,7 +37,7 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
-constexpr int kWaves = 4;                  // per block
+constexpr int NW = 8, kThreads = NW * 64;  // waves and threads of a block: one block to a compute unit, two waves to a SIMD
 
 // What a page holds and what the queries are.
 enum { P_F32 = 0, P_F16, P_BF16, P_E4M3_F16, P_E4M3_BF16 };
@@ -53,7 +53,8 @@ template <int P> struct Form {
     // f16 weights are taken 2^8 times as large, so that what is lost below the type's range is 2^-32 of the largest one
     static constexpr float BIAS = F16V ? 8.f : 0.f;
 };
-constexpr float kSlack = 7.f;              // the reference moves when a logit exceeds it by 2^7: seldom after the first tiles
+constexpr int kSoloTiles = 4;              // a pair of so many tiles at most is one wave's
+constexpr float kSlack = 7.f;               // the reference moves when a logit exceeds it by 2^7: seldom after the first tiles
 
 __device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float scale_of(unsigned e) { return __uint_as_float(e << 23); }        // 2^(e - 127), e 1 .. 254
@@ -96,125 +97,204 @@ template <bool F16> __device__ inline int pack(float x, float y, float left)
     }
 }
 
-// the other lane of 8 in a row of 16
-__device__ inline float across8(float v)
+// Lane moves within the wave that need no LDS: a row is 16 lanes.
+template <int CTRL, int ROWS> __device__ inline int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, CTRL < 0x120); }
+__device__ inline float across8(float v) { return __builtin_bit_cast(float, dpp<0x128, 0xf>(__builtin_bit_cast(int, v))); }   // the lane 8 away in the row
+// the maximum / sum over the four lanes of the same column (the same place in the four rows)
+template <class Op> __device__ inline float column(float v, Op op)
 {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x128, 0xf, 0xf, false));   // row_ror:8
+    const unsigned x = __float_as_uint(v);
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const unsigned y = __float_as_uint(op(__uint_as_float(r[0]), __uint_as_float(r[1])));
+    const auto s = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
-// the maximum / sum over the four lanes of the same column
-__device__ inline float column_max(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
-__device__ inline float column_sum(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
-
-// a value that all lanes agree on, in scalar registers
-__device__ inline uint64_t uniform(uint64_t v)
+__device__ inline float column_max(float v) { return column(v, [](float x, float y) { return fmaxf(x, y); }); }
+__device__ inline float column_sum(float v) { return column(v, [](float x, float y) { return x + y; }); }
+// op over the lanes up to this one; 0 is op's neutral element
+template <class Op> __device__ inline int scan(int v, Op op)
 {
-    return (uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+    v = op(v, dpp<0x111, 0xf>(v));         // row_shr 1, 2, 4, 8
+    v = op(v, dpp<0x112, 0xf>(v));
+    v = op(v, dpp<0x114, 0xf>(v));
+    v = op(v, dpp<0x118, 0xf>(v));
+    v = op(v, dpp<0x142, 0xa>(v));         // the last lane of row 0 to row 1, of row 2 to row 3
+    return op(v, dpp<0x143, 0xc>(v));      // lane 31 to rows 2 and 3
 }
 
 // Partial results pass between the blocks of one launch as in the decode step over the bounded cache (attn_kernels.hip
 // gives the argument): device-scope stores, a wait for their acknowledgement, a block barrier, the ticket; and device-scope
 // loads behind the ticket.
 __device__ inline void publish(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ inline float acquire(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ inline float2 acquire2(const float* p)
+{
+    const uint64_t v = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+constexpr int kParts = 16;                 // partial results that the merging block asks for at a time
 
-// The running results of one wave: lane (m, q) has column m of rows 4 q .. 4 q + 3 of each 16 output dimensions.
-template <int D> struct WaveState {
-    f32x4 o[D / 16];
-    float sum, ref;
-    bool bad;                              // a page number that is none was met
+// A block barrier that orders LDS alone: loads and stores to memory stay under way.
+__device__ inline void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+__device__ inline i32x4 fetch(const void* p) { return __builtin_nontemporal_load((const i32x4*)p); }
+
+// A block's, or a wave's, share of one (sequence, head) pair: `count` of the pair's tiles from number `first` on.
+struct Segment {
+    int b, h;
+    Visible vis;
+    Tiles tiles;
+    uint32_t first, count;
+    __device__ inline int tile(uint32_t i) const { return tiles.at((int)(first + min(i, count - 1))); }   // number i of them, or the last
 };
 
-template <int P, int D> struct Attn {
+// One wave's way through its tiles of a segment.  The rows of the next tile are asked for as soon as the registers of the
+// present one are read: keys after the first product, values after the second, page numbers a tile ahead of that; so a wave
+// always has half a tile or more under way, in the registers of one.  (No branch lies between a load and the wait for it, or
+// the compiler would wait for all that are under way: the last tile, which asks for nothing, has code of its own.)
+// MASK: the cache has a window.
+template <int P, int D, bool MASK> struct Attn {
     using F = Form<P>;
     static constexpr int NC = D * F::EB / 64;          // 16-byte pieces of a key row per lane
     static constexpr int NT = F::KG / 4;               // products of 16 keys per tile
     static constexpr int NQ = P == P_F32 ? D / 16 : D / 32;   // 16-byte pieces of queries per lane
+    static constexpr int ROW = D * F::EB;
+    // Heads of 256 leave no registers for the queries: they stay in LDS, and every tile reads them from there.
+    static constexpr bool QLDS = D == 256;
+    struct Tile { int t0; int32_t pk, pv; };           // first key; pages of the keys that the lane loads of K, of V
 
-    // One lane's pieces of the query rows: column m is head m % 8 (fp32: m), zeros where there is none.
-    __device__ static inline void load_queries(const PagedAttnArgs& a, int b, int h, int lane, i32x4 (&q)[NQ])
+    const PagedAttnArgs& a;
+    const int lane, m, part;               // the lane is column m, rows 4 part .. 4 part + 3 of a product
+    i32x4* const ql;                       // [NQ][64 lanes]
+    i32x4 q[QLDS ? 1 : NQ], kk[NT][NC], vv[D / 16], ke, ve;
+    // The running results: column m of rows 4 part .. of each 16 output dimensions, relative to `ref`.
+    f32x4 o[D / 16];
+    float sum, ref;
+    bool bad;                              // a page number that is none was met
+
+    __device__ inline Attn(const PagedAttnArgs& args, i32x4* lds) : a(args), lane(threadIdx.x & 63), m(lane & 15), part(lane >> 4), ql(lds) {}
+
+    // Column m is head m % 8 (fp32: m), zeros where there is none.  Piece i covers what the product of the keys' pieces i
+    // (e4m3: half of piece i / 2) multiplies.
+    __device__ inline const char* query_row(const Segment& s) const
     {
-        const int g = lane & (P == P_F32 ? 15 : 7), part = lane >> 4;
-        const char* row = a.q + (int64_t)b * a.q_seq + (int64_t)(h * a.G + g) * a.q_head;
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            // piece i covers what the product of the keys' pieces i (e4m3: half of piece i / 2) multiplies
-            const int at = F::E4M3 ? (i / 2) * 128 + part * 32 + (i & 1) * 16 : i * 64 + part * 16;
-            q[i] = g < a.G ? *(const i32x4*)(row + at) : i32x4{0, 0, 0, 0};
-        }
+        const int g = P == P_F32 ? m : m & 7;
+        return a.q + (int64_t)s.b * a.q_seq + (int64_t)(s.h * a.G + min(g, a.G - 1)) * a.q_head + (F::E4M3 ? part * 32 : part * 16);
+    }
+    __device__ inline i32x4 query_piece(const char* row, int i) const
+    {
+        const i32x4 x = *(const i32x4*)(row + (F::E4M3 ? (i / 2) * 128 + (i & 1) * 16 : i * 64));
+        return (P == P_F32 ? m : m & 7) < a.G ? x : i32x4{0, 0, 0, 0};
     }
 
-    __device__ static inline void tile(const PagedAttnArgs& a, const int32_t* table_row, const Visible& vis, int h, int t0,
-                                       int lane, const i32x4 (&q)[NQ], WaveState<D>& w)
+    // First of the KG keys that the lane loads of K, of V.
+    __device__ inline int key_group(int t0) const { return t0 + F::KG * (m >> 2); }
+    __device__ inline int value_group(int t0) const { return t0 + F::KG * part; }
+    // Their page: of a group of which no key is visible that of the sequence's last key, which always is.
+    __device__ inline int32_t page_of_group(const Segment& s, int first) const
     {
-        const int m = lane & 15, part = lane >> 4;
-        const int gk = t0 + F::KG * (m >> 2), gv = t0 + F::KG * part;    // first of the KG keys that the lane loads of K, of V
-        // Pages.  Groups of keys of which none is visible are not looked up; their rows are page 0's, masked below.
-        auto page = [&](int first) {
-            const bool any = first < vis.length && (first + F::KG > vis.from || first < vis.sink_end);
-            int pg = any ? page_of(table_row, first, a.pages.rows_log2, a.pages.n_pages) : 0;
-            if (pg < 0) { w.bad = true; pg = 0; }
-            return (int64_t)pg * a.pages.heads + h;
-        };
-        const int64_t pk = page(gk), pv = page(gv);
-        const int R = a.pages.rows, in_k = gk & (R - 1), in_v = gv & (R - 1);
-        const char* krow = a.pages.k + (pk * R + in_k + (m & 3)) * (D * F::EB) + part * 16;
-        const char* vcol = a.pages.v + (pv * R + in_v) * (D * F::EB) + m * 16;
-        i32x4 kk[NT][NC], vv[D / 16];
+        int j = min(first, s.vis.length - 1);
+        if constexpr (MASK)
+            if (first + F::KG <= s.vis.from && first >= s.vis.sink_end) j = s.vis.length - 1;
+        return a.pages.table[(int64_t)s.b * a.pages.cols + (j >> a.pages.rows_log2)];
+    }
+    __device__ inline Tile look_up(const Segment& s, uint32_t i) const
+    {
+        const int t0 = s.tile(i) * F::TILE;
+        return Tile{t0, page_of_group(s, key_group(t0)), page_of_group(s, value_group(t0))};
+    }
+    // A page's place and a row's within it; a page that is none stands for page 0, and is noted.
+    __device__ inline uint64_t page_at(int32_t pg)
+    {
+        const bool none = (unsigned)pg >= (unsigned)a.pages.n_pages;
+        bad |= none;
+        return (uint64_t)(unsigned)(none ? 0 : pg) * a.page_bytes;
+    }
+    __device__ inline uint32_t row_in_page(const Segment& s, int first) const { return (uint32_t)s.h * a.pages.rows + (first & (a.pages.rows - 1)); }
+    // (the keys' exponents come in the order of the logits: the lane's group of values)
+    __device__ inline void request_keys(const Segment& s, const Tile& t)
+    {
+        const char* p = a.pages.k + page_at(t.pk) + (row_in_page(s, key_group(t.t0)) + (m & 3)) * ROW + part * 16;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) kk[t][c] = *(const i32x4*)(krow + t * 4 * (D * F::EB) + c * 64);
-        i32x4 ke{}, ve{};
-        if constexpr (F::E4M3) {
-            ke = *(const i32x4*)(a.pages.k_exp + pv * R + in_v);
-            ve = *(const i32x4*)(a.pages.v_exp + pv * R + in_v);
-        }
+            for (int c = 0; c < NC; ++c) kk[i][c] = fetch(p + i * 4 * ROW + c * 64);
+        if constexpr (F::E4M3) ke = *(const i32x4*)(a.pages.k_exp + page_at(t.pv) / ROW + row_in_page(s, value_group(t.t0)));
+    }
+    __device__ inline void request_values(const Segment& s, const Tile& t)
+    {
+        const uint64_t page = page_at(t.pv);
+        const uint32_t row = row_in_page(s, value_group(t.t0));
+        if constexpr (F::E4M3) ve = *(const i32x4*)(a.pages.v_exp + page / ROW + row);
+        const char* p = a.pages.v + page + row * ROW + m * 16;
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) vv[d] = *(const i32x4*)(vcol + d * 256);
+        for (int d = 0; d < D / 16; ++d) vv[d] = fetch(p + d * 256);
+    }
 
-        f32x4 s[NT];
+    // logits of the tile's keys: s[t][e] is key value_group + 4 t + e of column m
+    __device__ inline void logits(f32x4 (&s)[NT]) const
+    {
+        int z = lane;
+        if constexpr (QLDS) asm volatile("" : "+v"(z));    // (or the compiler would take the reads out of the loop over the tiles)
+        auto query = [&](int i) { return QLDS ? ql[z + i * 64] : q[QLDS ? 0 : i]; };
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if constexpr (P == P_F32) {
+        for (int c = 0; c < NC; ++c) {
+            if constexpr (P == P_F32) {
+                const i32x4 x = query(c);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (int)kk[t][c][e]), __builtin_bit_cast(float, (int)q[c][e]), s[t], 0, 0, 0);
-                } else if constexpr (F::E4M3) {
-                    s[t] = mma<F::F16Q>(widen<F::F16Q>(kk[t][c], 0), q[2 * c], s[t]);
-                    s[t] = mma<F::F16Q>(widen<F::F16Q>(kk[t][c], 1), q[2 * c + 1], s[t]);
-                } else {
-                    s[t] = mma<F::F16Q>(kk[t][c], q[c], s[t]);
+                for (int e = 0; e < 4; ++e)
+                    s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (int)kk[0][c][e]), __builtin_bit_cast(float, (int)x[e]), s[0], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int hf = 0; hf < (F::E4M3 ? 2 : 1); ++hf) {
+                    const i32x4 x = query(F::E4M3 ? 2 * c + hf : c);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        if constexpr (F::E4M3) s[t] = mma<F::F16Q>(widen<F::F16Q>(kk[t][c], hf), x, s[t]);
+                        else s[t] = mma<F::F16Q>(kk[t][c], x, s[t]);
+                    }
+                    if constexpr (QLDS) __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
-        const bool whole = t0 + F::TILE <= vis.length && (t0 >= vis.from || t0 + F::TILE <= vis.sink_end);
+    }
+
+    // weights of the tile's keys and their sum with the values
+    __device__ inline void accumulate(const Visible& vis, int t0, f32x4 (&s)[NT], i32x4 exps)
+    {
+        const bool whole = t0 + F::TILE <= vis.length && (!MASK || t0 >= vis.from || t0 + F::TILE <= vis.sink_end);
+        uint32_t seen = ~0u;
+        if (!whole) seen = MASK ? vis.bits(value_group(t0), F::KG) : Visible::below(vis.length - value_group(t0), F::KG);
         float top = -INFINITY;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 float x = s[t][e] * a.scale_log2;
-                if constexpr (F::E4M3) x *= scale_of(((unsigned)ke[t] >> (8 * e)) & 255u);
-                if (!whole && !vis.sees(gv + 4 * t + e)) x = -INFINITY;
+                if constexpr (F::E4M3) x *= scale_of(((unsigned)exps[t] >> (8 * e)) & 255u);
+                if (!((seen >> (4 * t + e)) & 1)) x = -INFINITY;
                 s[t][e] = x;
                 top = fmaxf(top, x);
             }
-        if (__any(top > w.ref + (F::BIAS + kSlack))) {
-            const float moved = fmaxf(w.ref, column_max(top) - F::BIAS), by = fast_exp2(w.ref - moved);
-            w.sum *= by;
+        if (__any(top > ref + (F::BIAS + kSlack))) {
+            const float moved = fmaxf(ref, column_max(top) - F::BIAS), by = fast_exp2(ref - moved);
+            sum *= by;
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d) w.o[d] *= by;
-            w.ref = moved;
+            for (int d = 0; d < D / 16; ++d) o[d] *= by;
+            ref = moved;
         }
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[t][e] = fast_exp2(s[t][e] - w.ref);
-                w.sum += s[t][e];
+                s[t][e] = fast_exp2(s[t][e] - ref);
+                sum += s[t][e];
             }
         // What a masked place of V holds must not matter: a weight of 0 does not cancel a NaN.
         if (!whole) {
@@ -223,7 +303,7 @@ template <int P, int D> struct Attn {
                 unsigned keep = 0;
 #pragma unroll
                 for (int e = 0; e < F::KG / 4; ++e)
-                    if (vis.sees(gv + i * (F::KG / 4) + e)) keep |= (F::EB == 4 ? ~0u : F::EB == 2 ? 0xffffu << (16 * e) : 0xffu << (8 * e));
+                    if ((seen >> (i * (F::KG / 4) + e)) & 1) keep |= (F::EB == 4 ? ~0u : F::EB == 2 ? 0xffffu << (16 * e) : 0xffu << (8 * e));
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) vv[d][i] &= (int)keep;
                 if constexpr (F::E4M3) ve[i] &= (int)keep;
@@ -234,7 +314,7 @@ template <int P, int D> struct Attn {
             for (int d = 0; d < D / 16; ++d)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    w.o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (int)vv[d][e]), s[0][e], w.o[d], 0, 0, 0);
+                    o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (int)vv[d][e]), s[0][e], o[d], 0, 0, 0);
         } else {
             const float left = m < 8 ? 0.f : 1.f;
             if constexpr (F::E4M3) {
@@ -249,148 +329,332 @@ template <int P, int D> struct Attn {
                                  pack<F::F16V>(s[2 * hf + 1][0], s[2 * hf + 1][1], left), pack<F::F16V>(s[2 * hf + 1][2], s[2 * hf + 1][3], left)};
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) {
-                    if constexpr (F::E4M3) w.o[d] = mma<false>(widen<false>(vv[d], hf), p, w.o[d]);
-                    else w.o[d] = mma<F::F16V>(vv[d], p, w.o[d]);
+                    if constexpr (F::E4M3) o[d] = mma<false>(widen<false>(vv[d], hf), p, o[d]);
+                    else o[d] = mma<F::F16V>(vv[d], p, o[d]);
+                    if constexpr (D == 256 && F::E4M3) if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
     }
+
+    // Tiles i, i + step, .. of the segment; afterwards columns 0 .. 7 hold the heads' results (fp32: all columns do).
+    __device__ inline void run(const Segment& s, uint32_t i, uint32_t step, int wave)
+    {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        sum = 0.f;
+        ref = -3e38f;
+        bad = s.vis.length < 0;
+        if constexpr (QLDS) {
+            if (s.count > 0) {
+                const char* row = query_row(s);
+                for (int x = wave; x < NQ; x += NW) ql[x * 64 + lane] = query_piece(row, x);
+            }
+            lds_barrier();
+        }
+        if (i < s.count) {
+            Tile t = look_up(s, i), next = look_up(s, i + step);
+            if constexpr (!QLDS) {
+                const char* row = query_row(s);
+#pragma unroll
+                for (int x = 0; x < NQ; ++x) q[x] = query_piece(row, x);
+            }
+            request_keys(s, t);
+            request_values(s, t);
+            f32x4 x[NT];
+            for (; i + step < s.count; i += step) {
+                const i32x4 exps = ke;
+                logits(x);
+                const Tile after = look_up(s, i + 2 * step);
+                __builtin_amdgcn_sched_barrier(0);
+                request_keys(s, next);
+                __builtin_amdgcn_sched_barrier(0);
+                accumulate(s.vis, t.t0, x, exps);
+                __builtin_amdgcn_sched_barrier(0);
+                request_values(s, next);
+                __builtin_amdgcn_sched_barrier(0);
+                t = next;
+                next = after;
+            }
+            logits(x);
+            accumulate(s.vis, t.t0, x, ke);
+        }
+        bad = __any(bad);
+        sum = column_sum(sum);
+        if (bad) sum = __builtin_nanf("");
+        if constexpr (P != P_F32) {
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[d][e] += across8(o[d][e]);
+        }
+    }
 };
 
-template <int P, int D>
-__global__ __launch_bounds__(kWaves * 64) void paged_attn_kernel(const PagedAttnArgs a)
+// What is needed at the end only is fetched there: in scalar registers all along, it would crowd out what the loop needs.
+typedef const __attribute__((address_space(4))) PagedAttnArgs* LateArgs;
+__device__ inline LateArgs late_args()
+{
+    LateArgs p = (LateArgs)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
+// What this block has published before is there for whoever draws a later number from `counter`: true for the block that
+// draws the last of `count`, which may then read what the others have published, and which resets the counter.
+__device__ inline bool last_to_arrive(int32_t* counter, int count, int* shared)
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0): this wave's partial results are acknowledged
+    lds_barrier();
+    if (threadIdx.x == 0) {
+        const int before = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == count - 1) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next step
+        *shared = before;
+    }
+    lds_barrier();
+    const bool last = __builtin_amdgcn_readfirstlane(*shared) == count - 1;
+    if (last) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    return last;
+}
+
+struct Sum2 { float ref, sum; float2 o; };             // of two output elements
+
+// A pair of which this block has only a part: publishes the part, and in the block that finishes last for the pair (for the
+// part's group first, where there are many) adds up all of them in order.  A thread takes two output elements; the heads are
+// laid over the threads as often as they fit, as teams that share the parts.  kParts parts are asked for at a time: one after
+// the other, each would wait for memory.
+template <int D> __device__ inline void join_parts(const Parts& all, int slot, int64_t unit, const float2 (&stat)[NW][8], float (&acc)[NW][8][D], int* arrived)
+{
+    constexpr int HT = D / 2, HL = HT < 64 ? HT : 64;  // threads of a head; lanes of a wave that work on one head
+    constexpr int NH = kThreads / HT;                  // heads that the block has threads for
+    LateArgs a = late_args();
+    const int tid = threadIdx.x, lane = tid & 63, j = lane % HL, G = a->G, e = tid % HT * 2;
+    float* const part_o = a->part_o;
+    float* const part_ml = a->part_ml;
+    const int padded = G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : 8, teams = padded < NH ? NH / padded : 1;
+    const int group = group_of(all.parts);
+    bool last = group == 1;
+    int first = last ? 0 : ((int)blockIdx.x - all.from) / group * group, stride = 1, count = last ? all.parts : min(group, all.parts - first), to = all.slot(first);
+    while (last_to_arrive(last ? a->ticket + unit : a->group_ticket + to, count, arrived)) {
+        for (int g0 = 0; g0 < G; g0 += NH) {
+            const int g = g0 + (tid / HT & (padded < NH ? padded - 1 : NH - 1)), team = tid / HT / padded;
+            Sum2 s{-3e38f, 0.f, make_float2(0.f, 0.f)};
+            if (g < G) {
+                for (int p0 = team; p0 < count; p0 += kParts * teams) {
+                    // lane j of a head's lanes fetches the (reference, sum) of its team's part p0 + j
+                    auto at = [&](int k) { return (all.slot(first + min(p0 + k * teams, count - 1) * stride) * G + g); };
+                    const bool have = j < kParts && p0 + j * teams < count;
+                    const float2 ml = acquire2(part_ml + at(j % kParts) * 2);
+                    float2 x[kParts];
+#pragma unroll
+                    for (int k = 0; k < kParts; k += 4) {
+                        if (p0 + k * teams >= count) break;
+#pragma unroll
+                        for (int i = k; i < k + 4; ++i) x[i] = acquire2(part_o + at(i) * D + e);
+                    }
+                    float ref = have ? ml.x : -3e38f;
+#pragma unroll
+                    for (int d = 1; d < kParts; d <<= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
+                    ref = fmaxf(s.ref, __shfl(ref, lane - j));
+                    const float by = have ? fast_exp2(ml.x - ref) : 0.f, old = fast_exp2(s.ref - ref);
+                    s.sum *= old; s.o.x *= old; s.o.y *= old; s.ref = ref;
+#pragma unroll
+                    for (int k = 0; k < kParts; ++k) {
+                        if (p0 + k * teams >= count) break;
+                        const float b = __shfl(by, lane - j + k);
+                        s.sum = fmaf(b, __shfl(ml.y, lane - j + k), s.sum);
+                        s.o.x = fmaf(b, x[k].x, s.o.x);
+                        s.o.y = fmaf(b, x[k].y, s.o.y);
+                    }
+                }
+            }
+            Sum2* sums = (Sum2*)&acc[0][0][0];
+            __syncthreads();                           // all have read what emitting a group's sum may overwrite
+            if (teams > 1) {
+                sums[tid] = s;
+                lds_barrier();
+                if (team == 0)
+                    for (int t = 1; t < teams; ++t) {
+                        const Sum2 x = sums[tid + t * padded * HT];
+                        const float ref = fmaxf(s.ref, x.ref), u = fast_exp2(s.ref - ref), v = fast_exp2(x.ref - ref);
+                        s = Sum2{ref, fmaf(s.sum, u, x.sum * v), make_float2(fmaf(s.o.x, u, x.o.x * v), fmaf(s.o.y, u, x.o.y * v))};
+                    }
+            }
+            if (team == 0 && g < G) {
+                if (last) {
+                    *(float2*)(a->out + (unit * G + g) * D + e) = make_float2(s.o.x / s.sum, s.o.y / s.sum);
+                    if (e == 0 && a->lse) a->lse[unit * G + g] = (s.ref + log2f(s.sum)) * 0.6931471805599453f;
+                } else {
+                    const int64_t row = (int64_t)to * G + g;
+                    publish(part_o + row * D + e, s.o.x);
+                    publish(part_o + row * D + e + 1, s.o.y);
+                    if (e == 0) { publish(part_ml + row * 2, s.ref); publish(part_ml + row * 2 + 1, s.sum); }
+                }
+            }
+        }
+        if (last) break;
+        last = true;
+        first = 0; stride = group; count = (all.parts + group - 1) / group;
+    }
+}
+
+template <int P, int D, bool MASK>
+__global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArgs a)
 {
     using F = Form<P>;
-    using A = Attn<P, D>;
-    __shared__ float acc[kWaves][8][D];
-    __shared__ float2 stat[kWaves][8];     // (reference, sum)
+    using A = Attn<P, D, MASK>;
+    __shared__ float acc[NW][8][D];
+    __shared__ float2 stat[NW][8];         // (reference, sum)
+    __shared__ i32x4 queries[A::QLDS ? A::NQ * 64 : 1];
     __shared__ int arrived;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), G = a.G, H = a.pages.heads;
-    const int64_t most = (int64_t)a.pages.cols * a.pages.rows;
-    // A pair without visible keys, or with a length that is none, counts as one tile: somebody has to write its output.
-    auto tiles_in = [&](int b) {
-        const int n = tiles_of(visible(a.length[b], a.sink, a.window, most), F::TILE).count;
-        return (uint64_t)(n > 0 ? n : 1) * (unsigned)H;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), H = a.pages.heads;
+    const int32_t most = a.pages.cols << a.pages.rows_log2;
+    auto visible_in = [&](int length) {
+        if constexpr (MASK) return visible(length, a.sink, a.window, most);
+        else return Visible{length > most ? -1 : length, 0, 0};
     };
-    // Every wave adds up the tiles of all sequences, `per` consecutive ones to a lane.
+    auto tiles_in = [&](const Visible& v) {
+        if constexpr (MASK) return tiles_of(v, F::TILE);
+        else return Tiles{0, 0, v.length > 0 ? (int)((uint32_t)(v.length - 1) / F::TILE) + 1 : 0};
+    };
+    // Every wave looks at the lengths of all sequences, `per` consecutive ones to a lane.
     const int per = (a.batch + 63) / 64;
-    uint64_t mine = 0;
-    for (int i = lane * per; i < min((lane + 1) * per, a.batch); ++i) mine += tiles_in(i);
-    uint64_t upto = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t x = __shfl_up(upto, o);
-        if (lane >= o) upto += x;
+    int one = 0;                           // the lane's length, where each has one
+    uint32_t mine = 0;
+    int longest = 0;
+    if (per == 1) {
+        one = a.length[min(lane, a.batch - 1)];
+        longest = tiles_in(visible_in(one)).count;
+        mine = lane < a.batch ? units_of(longest) : 0;
+    } else {
+        for (int i = lane * per; i < min((lane + 1) * per, a.batch); ++i) {
+            const int n = tiles_in(visible_in(a.length[i])).count;
+            longest = max(longest, n);
+            mine += units_of(n);
+        }
     }
-    const uint64_t total = uniform(__shfl(upto, 63));
-    const uint64_t share = tiles_per_block(total, gridDim.x);
-    uint64_t cur = share * blockIdx.x;
-    if (cur >= total) return;
-    const uint64_t end = min(cur + share, total);
-    const int owner = __ffsll((unsigned long long)__ballot(cur < upto)) - 1;
-    uint64_t off = uniform(cur - __shfl(upto - mine, owner));   // tiles between the start of sequence b and the block's first
-    int b = owner * per;
-    for (uint64_t n; off >= (n = tiles_in(b)); ++b) off -= n;
+    longest = __builtin_amdgcn_readlane(scan(longest, [](int x, int y) { return max(x, y); }), 63);
+    auto segment = [&](int b, int h) {
+        Segment s;
+        s.b = b;
+        s.h = h;
+        s.vis = visible_in(per == 1 ? __builtin_amdgcn_readlane(one, b) : __builtin_amdgcn_readfirstlane(a.length[b]));
+        s.tiles = tiles_in(s.vis);
+        s.first = 0;
+        s.count = s.tiles.count;
+        return s;
+    };
+    A w(a, queries);
 
-    while (cur < end) {
-        const Visible vis = visible(a.length[b], a.sink, a.window, most);
-        const Tiles tiles = tiles_of(vis, F::TILE);
-        const unsigned n = tiles.count > 0 ? tiles.count : 1;
-        const int h = (int)(off / n);
-        const unsigned first = (unsigned)(off - (uint64_t)h * n);
-        const unsigned here = (unsigned)min((uint64_t)(n - first), end - cur);
-        const int32_t* table_row = a.pages.table + (int64_t)b * a.pages.cols;
-
-        WaveState<D> w;
+    // Pairs of a few tiles: a wave to each, which needs nobody else.
+    if (!A::QLDS && longest <= kSoloTiles) {
+        for (uint32_t pair = wave * gridDim.x + blockIdx.x; pair < (uint32_t)a.batch * H; pair += gridDim.x * NW) {   // over all compute units first
+            const Segment s = segment(pair / H, pair % H);
+            w.run(s, 0, 1, wave);
+            LateArgs l = late_args();
+            const int G = l->G;
+            if (w.m < G) {
+                const int64_t row = (int64_t)pair * G + w.m;
+                const bool any = s.count > 0;
+                float* out = l->out + row * D + w.part * 4;
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) w.o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-        w.sum = 0.f; w.ref = -3e38f; w.bad = vis.length < 0;
-        if (tiles.count > 0) {
-            i32x4 q[A::NQ];
-            A::load_queries(a, b, h, lane, q);
-            for (unsigned i = wave; i < here; i += kWaves)
-                A::tile(a, table_row, vis, h, tiles.at(first + i) * F::TILE, lane, q, w);
-        }
-        const bool bad = __any(w.bad);
-        w.sum = column_sum(w.sum);
-        const int m = lane & 15, part = lane >> 4;
+                for (int d = 0; d < D / 16; ++d) {
+                    f32x4 x;
 #pragma unroll
-        for (int d = 0; d < D / 16; ++d) {
-            f32x4 x = w.o[d];
-            if constexpr (P != P_F32) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] += across8(x[e]);
+                    for (int e = 0; e < 4; ++e) x[e] = any ? w.o[d][e] / w.sum : w.sum;   // nothing visible: 0, or NaN
+                    *(f32x4*)(out + d * 16) = x;
+                }
+                if (w.part == 0 && l->lse) l->lse[row] = any ? (w.ref + log2f(w.sum)) * 0.6931471805599453f : w.sum - INFINITY;
             }
-            if (m < G) *(f32x4*)&acc[wave][m][d * 16 + part * 4] = x;
         }
-        if (part == 0 && m < G) stat[wave][m] = make_float2(w.ref, bad ? __builtin_nanf("") : w.sum);
-        __syncthreads();
+        return;
+    }
 
-        const bool alone = first == 0 && here == n;
-        const int64_t unit = (int64_t)b * H + h;
-        const int64_t slot = 2 * (int64_t)blockIdx.x + (first == 0 ? 1 : 0);
-        for (int i = tid; i < G * D; i += kWaves * 64) {
+    const bool split = longest > kWholeTiles;
+    if (!split) mine = max(0, min(per, a.batch - lane * per));
+    const uint32_t upto = scan(mine, [](int x, int y) { return x + y; });
+    const uint32_t total = __builtin_amdgcn_readlane(upto, 63) * (uint32_t)H, share = units_per_block(total, gridDim.x);
+    uint32_t cur = share * blockIdx.x;
+    if (cur >= total) return;
+    const uint32_t end = min(cur + share, total);
+    const int owner = __ffsll((unsigned long long)__ballot(cur < upto * H)) - 1;
+    uint32_t off = cur - __builtin_amdgcn_readlane(upto - mine, owner) * H;   // units between the start of sequence b and the block's first
+    int b = owner * per;
+    auto units = [&](const Segment& s) { return split ? units_of(s.tiles.count) : 1u; };
+    if (per > 1)
+        for (uint32_t n; off >= (n = units(segment(b, 0)) * H); ++b) off -= n;
+
+    while (true) {
+        Segment s = segment(b, 0);
+        const uint32_t n = units(s);
+        s.h = off / n;
+        const uint32_t first = off - s.h * n, here = min(n - first, end - cur);
+        if (split && s.count > 0) {
+            s.first = first * kUnitTiles;
+            s.count = min(here * kUnitTiles, s.tiles.count - s.first);
+        }
+        w.run(s, wave, NW, wave);
+        LateArgs l = late_args();
+        const int G = l->G;
+        if (w.m < G) {
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) *(f32x4*)&acc[wave][w.m][d * 16 + w.part * 4] = w.o[d];
+            if (w.part == 0) stat[wave][w.m] = make_float2(w.ref, w.sum);
+        }
+        lds_barrier();
+
+        const bool alone = here == n, any = s.tiles.count > 0;
+        const int64_t unit = (int64_t)b * H + s.h;
+        const int slot = 2 * (int)blockIdx.x + (first == 0 ? 1 : 0);
+        for (int i = tid; i < G * D; i += kThreads) {
             const int g = i / D, d = i - g * D;
             float ref = stat[0][g].x, sum = 0.f, o = 0.f;
 #pragma unroll
-            for (int x = 1; x < kWaves; ++x) ref = fmaxf(ref, stat[x][g].x);
+            for (int x = 1; x < NW; ++x) ref = fmaxf(ref, stat[x][g].x);
 #pragma unroll
-            for (int x = 0; x < kWaves; ++x) {
+            for (int x = 0; x < NW; ++x) {
                 const float by = fast_exp2(stat[x][g].x - ref);
                 sum = fmaf(by, stat[x][g].y, sum);
                 o = fmaf(by, acc[x][g][d], o);
             }
             if (alone) {
-                a.out[unit * G * D + i] = tiles.count > 0 ? o / sum : sum;       // nothing visible: 0, or NaN
-                if (d == 0 && a.lse) a.lse[unit * G + g] = tiles.count > 0 ? (ref + log2f(sum)) * 0.6931471805599453f : sum - INFINITY;
+                l->out[unit * G * D + i] = any ? o / sum : sum;                  // nothing visible: 0, or NaN
+                if (d == 0 && l->lse) l->lse[unit * G + g] = any ? (ref + log2f(sum)) * 0.6931471805599453f : sum - INFINITY;
             } else {
-                publish(a.part_o + slot * G * D + i, o);
-                if (d == 0) { publish(a.part_ml + (slot * G + g) * 2, ref); publish(a.part_ml + (slot * G + g) * 2 + 1, sum); }
+                publish(l->part_o + (int64_t)slot * G * D + i, o);
+                if (d == 0) { publish(l->part_ml + ((int64_t)slot * G + g) * 2, ref); publish(l->part_ml + ((int64_t)slot * G + g) * 2 + 1, sum); }
             }
         }
-        if (!alone) {
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-            __builtin_amdgcn_s_waitcnt(0x0F70);        // vmcnt(0): this wave's partial results are acknowledged
-            __syncthreads();
-            const Parts all = parts_of(cur - first, n, share);
-            if (tid == 0) arrived = __hip_atomic_fetch_add(a.ticket + unit, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __syncthreads();
-            if (__builtin_amdgcn_readfirstlane(arrived) == all.parts - 1) {
-                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
-                for (int i = tid; i < G * D; i += kWaves * 64) {
-                    const int g = i / D, d = i - g * D;
-                    float ref = -3e38f, sum = 0.f, o = 0.f;
-                    for (int p = 0; p < all.parts; ++p) {
-                        const int64_t s = all.slot(p);
-                        const float r = acquire(a.part_ml + (s * G + g) * 2), l = acquire(a.part_ml + (s * G + g) * 2 + 1);
-                        const float x = acquire(a.part_o + s * G * D + i);
-                        const float moved = fmaxf(ref, r), old = fast_exp2(ref - moved), by = fast_exp2(r - moved);
-                        sum = fmaf(sum, old, by * l);
-                        o = fmaf(o, old, by * x);
-                        ref = moved;
-                    }
-                    a.out[unit * G * D + i] = o / sum;
-                    if (d == 0 && a.lse) a.lse[unit * G + g] = (ref + log2f(sum)) * 0.6931471805599453f;
-                }
-                if (tid == 0) __hip_atomic_store(a.ticket + unit, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // ready for the next step
-            }
-        }
-        __syncthreads();                               // the next pair's results go to the same LDS
+        if (!alone) join_parts<D>(parts_of(cur - first, n, share), slot, unit, stat, acc, &arrived);
         cur += here;
+        if (cur >= end) break;
         off += here;
-        if (off == (uint64_t)n * (unsigned)H) { off = 0; ++b; }
+        if (off == n * H) { off = 0; ++b; }
+        lds_barrier();                                 // the next pair's results go to the same LDS
     }
 }
 
-template <int P> hipError_t launch(const PagedAttnArgs& a, int grid, hipStream_t st)
+template <int P, int D> hipError_t launch(const PagedAttnArgs& a, int compute_units, hipStream_t st)
+{
+    int64_t grid = compute_units < kPagedMaxBlocks ? compute_units : kPagedMaxBlocks;
+    // no more blocks than could have units
+    constexpr int unit = Form<P>::TILE * kUnitTiles;
+    const int64_t units = (int64_t)a.batch * a.pages.heads * (((int64_t)a.pages.cols * a.pages.rows + unit - 1) / unit);
+    if (grid > units) grid = units;
+    if (a.window > 0) hipLaunchKernelGGL((paged_attn_kernel<P, D, true>), dim3((unsigned)grid), dim3(kThreads), 0, st, a);
+    else hipLaunchKernelGGL((paged_attn_kernel<P, D, false>), dim3((unsigned)grid), dim3(kThreads), 0, st, a);
+    return hipGetLastError();
+}
+
+template <int P> hipError_t launch(const PagedAttnArgs& a, int compute_units, hipStream_t st)
 {
     switch (a.pages.D) {
-        case 64: hipLaunchKernelGGL((paged_attn_kernel<P, 64>), dim3(grid), dim3(kWaves * 64), 0, st, a); break;
-        case 128: hipLaunchKernelGGL((paged_attn_kernel<P, 128>), dim3(grid), dim3(kWaves * 64), 0, st, a); break;
-        case 256: hipLaunchKernelGGL((paged_attn_kernel<P, 256>), dim3(grid), dim3(kWaves * 64), 0, st, a); break;
-        default: return hipErrorInvalidValue;
+        case 64: return launch<P, 64>(a, compute_units, st);
+        case 128: return launch<P, 128>(a, compute_units, st);
+        case 256: return launch<P, 256>(a, compute_units, st);
     }
-    return hipGetLastError();
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -398,15 +662,9 @@ template <int P> hipError_t launch(const PagedAttnArgs& a, int grid, hipStream_t
 hipError_t launch_paged_attn(int dtype, int page_dtype, const PagedAttnArgs& a, int compute_units, hipStream_t st)
 {
     const bool e4m3 = page_dtype == BUZZ_E4M3;
-    const int tile = e4m3 ? 64 : dtype == BUZZ_FP32 ? 16 : 32;
-    int64_t grid = (int64_t)compute_units * 2;
-    if (grid > kPagedMaxBlocks) grid = kPagedMaxBlocks;
-    // no more blocks than could have tiles, four to a block
-    const int64_t most = ((int64_t)a.pages.cols * a.pages.rows + tile - 1) / tile, tiles = (int64_t)a.batch * a.pages.heads * (most > 0 ? most : 1);
-    if (grid > (tiles + kWaves - 1) / kWaves) grid = (tiles + kWaves - 1) / kWaves;
-    if (dtype == BUZZ_FP32) return launch<P_F32>(a, (int)grid, st);
-    if (dtype == BUZZ_FP16) return e4m3 ? launch<P_E4M3_F16>(a, (int)grid, st) : launch<P_F16>(a, (int)grid, st);
-    return e4m3 ? launch<P_E4M3_BF16>(a, (int)grid, st) : launch<P_BF16>(a, (int)grid, st);
+    if (dtype == BUZZ_FP32) return launch<P_F32>(a, compute_units, st);
+    if (dtype == BUZZ_FP16) return e4m3 ? launch<P_E4M3_F16>(a, compute_units, st) : launch<P_F16>(a, compute_units, st);
+    return e4m3 ? launch<P_E4M3_BF16>(a, compute_units, st) : launch<P_BF16>(a, compute_units, st);
 }
 
 }  // namespace buzz

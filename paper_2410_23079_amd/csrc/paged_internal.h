@@ -8,7 +8,7 @@
 
 namespace buzz {
 
-constexpr int kPagedMaxBlocks = 1024;      // blocks of a decode step; the workspace holds two partial results for each
+constexpr int kPagedMaxBlocks = 512;       // blocks of a decode step; the workspace holds two partial results for each
 constexpr int kPagedTileTokens = 16;       // positions that one block of the row kernels works on: every page is whole tiles
 
 struct Rows {                              // [sequence][head][row][head_dim], distances in bytes
@@ -51,6 +51,9 @@ __host__ __device__ inline int64_t tiles_of_rows(int64_t n) { return n <= 0 ? 0 
 struct Visible {
     int32_t length, from, sink_end;        // length < 0: the caller's length is none
     __host__ __device__ inline bool sees(int32_t j) const { return j < length && (j >= from || j < sink_end); }
+    // ... of the n <= 16 keys from j on, bit by bit
+    __host__ __device__ inline uint32_t bits(int32_t j, int32_t n) const { return below(sink_end - j, n) | (below(length - j, n) & ~below(from - j, n)); }
+    __host__ __device__ static inline uint32_t below(int32_t k, int32_t n) { return (1u << (k < 0 ? 0 : k > n ? n : k)) - 1u; }
 };
 __host__ __device__ inline Visible visible(int32_t length, int32_t sink, int32_t window, int64_t most)
 {
@@ -73,23 +76,30 @@ __host__ __device__ inline Tiles tiles_of(const Visible& v, int32_t tile)
     return Tiles{low, high, low + end - high};
 }
 
-// A decode step's tiles, numbered through over all (sequence, head) pairs, `share` consecutive ones to a block, four at
-// least (one per wave).  A pair of n tiles from number `begin` on is worked on by `parts` blocks from `from` on; each but the
-// one with the pair's first tile leaves its partial result in its slot 0, that one in slot 1, so a block that ends one pair
-// and begins another needs two.
-__host__ __device__ inline uint64_t tiles_per_block(uint64_t total, unsigned blocks)
-{
-    const uint64_t share = (total + blocks - 1) / blocks;
-    return share < 4 ? 4 : share;
-}
+// A decode step's work is cut into units of one (sequence, head) pair: kUnitTiles tiles, or the whole pair where no pair of the
+// step has more than kWholeTiles.  The units of all pairs are numbered through, `share` consecutive ones to a block.  A pair of n
+// units from number `begin` on is worked on by `parts` blocks from `from` on; each but the one with the pair's first unit leaves
+// its partial result in its slot 0, that one in slot 1, so a block that ends one pair and begins another needs two.
+constexpr int kUnitTiles = 4, kWholeTiles = 16;
+__host__ __device__ inline uint32_t units_of(int32_t tiles) { return tiles > 0 ? ((uint32_t)tiles + kUnitTiles - 1) / kUnitTiles : 1; }   // somebody has to write an empty pair's output
+__host__ __device__ inline uint32_t units_per_block(uint32_t total, uint32_t blocks) { return (total + blocks - 1) / blocks; }
 struct Parts {
     int from, parts;
-    __host__ __device__ inline int64_t slot(int i) const { return 2 * (int64_t)(from + i) + (i == 0 ? 1 : 0); }
+    __host__ __device__ inline int slot(int i) const { return 2 * (from + i) + (i == 0 ? 1 : 0); }
 };
-__host__ __device__ inline Parts parts_of(uint64_t begin, uint64_t n, uint64_t share)
+__host__ __device__ inline Parts parts_of(uint32_t begin, uint32_t n, uint32_t share)
 {
     const int from = (int)(begin / share);
     return Parts{from, (int)((begin + n - 1) / share) - from + 1};
+}
+// Partial results are added up sixteen or so at a time: those of a pair with more are added up by groups first.  Part i belongs
+// to the group of part i / group * group, whose slot takes the group's sum and numbers the group's arrival counter.
+__host__ __device__ inline int group_of(int parts) { return parts <= 16 ? 1 : parts <= 256 ? 16 : 32; }
+
+// Most units that a cache's configuration can lead to, of the smallest tiles (16 keys): they have to be countable in 31 bits.
+inline bool units_countable(int64_t batch, int64_t heads, int64_t cols, int64_t rows)
+{
+    return batch * heads <= INT32_MAX && (double)batch * (double)heads * (double)((cols * rows + 63) / 64) < 2147483648.0;
 }
 
 struct RotateArgs {
@@ -122,10 +132,12 @@ struct PagedAttnArgs {
     PageArgs pages;
     float* part_o;                         // [blocks][2][G][D] unnormalised outputs
     float* part_ml;                        // [blocks][2][G][2] (reference, sum)
-    int32_t* ticket;                       // [batch * heads], zero between launches
+    int32_t* ticket;                       // [batch * heads], arrivals of a pair's parts or groups; zero between launches
+    int32_t* group_ticket;                 // [2 * kPagedMaxBlocks], of a group's parts, by slot; likewise
     int32_t batch, G;
     int32_t sink, window;
     float scale_log2;
+    uint32_t page_bytes;                   // of one page of K, or of V: under 4 GiB
 };
 
 hipError_t launch_rotate(int dtype, int page_dtype, const RotateArgs& a, int batch, hipStream_t st);

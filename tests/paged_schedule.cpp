@@ -31,19 +31,20 @@ static void check_tiles(int length, int sink, int window, int tile, int64_t most
     for (int j = 0; j < length + tile; ++j) {
         const bool want = j < length && (window == 0 || j >= length - window || j < sink);
         CHECK(v.sees(j) == want);
+        for (int n : {4, 8, 16}) CHECK(((v.bits(j / n * n, n) >> (j % n)) & 1) == (uint32_t)want);
         if (want) CHECK(seen.count(j / tile * tile));
     }
     if (length == 0) CHECK(t.count == 0);
 }
 
-// The walk of the decode kernel's blocks over all tiles: each tile once, each pair's partial results in slots of their own
+// The walk of the decode kernel's blocks over all units: each unit once, each pair's partial results in slots of their own
 // within the workspace, as many arrivals as the merging block waits for.
 static void check_share(const std::vector<int>& n, int heads, unsigned blocks)
 {
     uint64_t total = 0;
     for (int x : n) total += (uint64_t)(x > 0 ? x : 1) * heads;
-    const uint64_t share = tiles_per_block(total, blocks);
-    std::vector<std::map<int64_t, int>> slots(n.size() * heads);     // pair -> slot -> tiles
+    const uint64_t share = units_per_block((uint32_t)total, blocks);
+    std::vector<std::map<int64_t, int>> slots(n.size() * heads);     // pair -> slot -> units
     std::vector<int> done(n.size() * heads, 0), alone(n.size() * heads, 0);
     std::set<int64_t> used;
     CHECK(share * blocks >= total);
@@ -66,7 +67,7 @@ static void check_share(const std::vector<int>& n, int heads, unsigned blocks)
                 const int64_t slot = 2 * (int64_t)block + (first == 0 ? 1 : 0);
                 CHECK(slot < 2 * kPagedMaxBlocks && used.insert(slot).second);
                 slots[pair][slot] = (int)here;
-                const Parts p = parts_of(cur - first, m, share);
+                const Parts p = parts_of((uint32_t)(cur - first), (uint32_t)m, (uint32_t)share);
                 bool mine = false;
                 for (int i = 0; i < p.parts; ++i) mine |= p.slot(i) == slot;
                 CHECK(mine);
@@ -77,6 +78,20 @@ static void check_share(const std::vector<int>& n, int heads, unsigned blocks)
             cur += here;
             off += here;
             if (off == m * heads) { off = 0; ++b; }
+        }
+    }
+    // groups of partial results: every part in one, whose slot is one of the pair's own
+    uint64_t begin = 0;
+    for (size_t pair = 0; pair < done.size(); ++pair) {
+        const uint64_t m = n[pair / heads] > 0 ? n[pair / heads] : 1;
+        const Parts all = parts_of((uint32_t)begin, (uint32_t)m, (uint32_t)share);
+        begin += m;
+        if (slots[pair].empty()) continue;
+        const int group = group_of(all.parts), groups = (all.parts + group - 1) / group;
+        CHECK(group <= 32 && groups <= 16 && (groups - 1) * group < all.parts && (group > 1 || groups == all.parts));
+        for (int i = 0; i < all.parts; ++i) {
+            CHECK(i / group < groups && slots[pair].count(all.slot(i / group * group)));
+            CHECK(all.slot(i) >= 0 && all.slot(i) < 2 * kPagedMaxBlocks);
         }
     }
     for (size_t pair = 0; pair < done.size(); ++pair) {
@@ -103,8 +118,10 @@ int main()
         check_share(n, 1 + upto(9), 1 + upto(i % 2 ? 40 : kPagedMaxBlocks));
     }
     check_share({0}, 1, 1);
-    check_share({1 << 24}, 1, kPagedMaxBlocks);
-    check_share(std::vector<int>(300, 1 << 24), 8, kPagedMaxBlocks);
+    check_share({1 << 22}, 1, kPagedMaxBlocks);
+    check_share(std::vector<int>(511, 1 << 22), 1, kPagedMaxBlocks);         // 2^31 - 2^22 units
+    CHECK(units_of(0) == 1 && units_of(1) == 1 && units_of(4) == 1 && units_of(5) == 2);
+    CHECK(units_countable(511, 1, 1 << 20, 256) && !units_countable(512, 1, 1 << 20, 256) && !units_countable(65535, 65535, 1, 16));
 
     // rows of a call: spans, and the tiles of 16 positions that cover them
     for (int i = 0; i < 3000; ++i) {

@@ -10,7 +10,7 @@ import torch
 
 from paper_2410_23079_amd import (FLAG_DRY_RUN, BuzzError, PagedCache, PagedConfig, Rotary, load_library,
                                   paged_workspace_bytes, qk_norm_rotate)
-from paper_2410_23079_amd.binding import _Pages, _Rotary, _Rows
+from paper_2410_23079_amd.binding import _Pages, _pack_rows, _Rotary
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HERE = os.path.join(ROOT, "tests")
@@ -48,12 +48,12 @@ def test_configurations_that_are_refused(bad, code):
 
 def test_the_workspace_holds_what_the_largest_step_leaves():
     c = cfg(n_q_heads=64, n_kv_heads=8, head_dim=256, batch=100)
-    # two partial results (max, sum, output) of 8 heads for each of 1024 blocks, and one counter for each pair
-    assert paged_workspace_bytes(c) >= 2 * 1024 * 8 * (256 + 2) * 4 + 100 * 8 * 4
+    # two partial results (max, sum, output) of 8 heads and their counters for each of 512 blocks, one counter for each pair
+    assert paged_workspace_bytes(c) >= 2 * 512 * 8 * (256 + 2) * 4 + 100 * 8 * 4 + 2 * 512 * 4
 
 
 def rows(ptr=0x1000, seq=4096, head=1024, row=128):
-    return _Rows(ptr, seq, head, row)
+    return _pack_rows(ptr or 0, seq, head, row)
 
 
 def dry(**kw):
@@ -80,7 +80,8 @@ def test_calls_that_are_refused():
     lib = load_library()
     c = dry()
     h, r = c._h, rows()
-    append = lambda n=4, batch=3, rot=None, q=None, q_out=None: lib.buzz_paged_append(h, rot, q, r, r, q_out, batch, n, 0x1000, None, None, None)
+    ref = lambda s: None if s is None else ctypes.byref(s)
+    append = lambda n=4, batch=3, rot=None, q=None, q_out=None: lib.buzz_paged_append(h, ref(rot), q, r, r, q_out, batch, n, 0x1000, None, None, None)
     assert append() == 0 and append(n=0) == 0 and append(batch=0) == 0
     assert append(n=-1) == -1 and append(batch=-1) == -1
     assert append(batch=4) == -2 and append(n=12 * 32 + 1) == -2                               # capacity
@@ -111,7 +112,7 @@ def test_rows_that_are_refused():
     lib, rot = load_library(), _Rotary(None, None, 0x1000, 1e-6, 64, 0, 0)
 
     def call(q=None, k=None, q_out=None, k_out=None, dtype=2, D=128, Hq=8, Hkv=2, rotary=rot, batch=2, n=4):
-        return lib.buzz_qk_norm_rotate(dtype, D, Hq, Hkv, rotary, q, k, q_out, k_out, batch, n, None, None, None)
+        return lib.buzz_qk_norm_rotate(dtype, D, Hq, Hkv, None if rotary is None else ctypes.byref(rotary), q, k, q_out, k_out, batch, n, None, None, None)
     r = rows()
     assert call() == 0 and call(r, r, r, r, batch=0) == 0 and call(r, r, r, r, n=0) == 0       # nothing to do
     assert call(r) == -1 and call(k=r) == -1 and call(q_out=r) == -1
