@@ -52,8 +52,10 @@ template <int P> struct Form {
                                                                           // their row's power of two, which f16 cannot hold
     // f16 weights are taken 2^8 times as large, so that what is lost below the type's range is 2^-32 of the largest one
     static constexpr float BIAS = F16V ? 8.f : 0.f;
+    // Tiles of a pair up to which one wave takes it: two, four where a tile costs little arithmetic; twice that where waves are
+    // hardly enough for the pairs.
+    static constexpr int SOLO = EB == 2 ? 4 : 2;
 };
-constexpr int kSoloTiles = 4;              // a pair of so many tiles at most is one wave's
 constexpr float kSlack = 7.f;               // the reference moves when a logit exceeds it by 2^7: seldom after the first tiles
 
 __device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -175,6 +177,7 @@ template <int P, int D, bool MASK> struct Attn {
     f32x4 o[D / 16];
     float sum, ref;
     bool bad;                              // a page number that is none was met
+    Tile t, next;                          // the tile that has been asked for, and the one after it
 
     __device__ inline Attn(const PagedAttnArgs& args, i32x4* lds) : a(args), lane(threadIdx.x & 63), m(lane & 15), part(lane >> 4), ql(lds) {}
 
@@ -337,13 +340,9 @@ template <int P, int D, bool MASK> struct Attn {
         }
     }
 
-    // Tiles i, i + step, .. of the segment; afterwards columns 0 .. 7 hold the heads' results (fp32: all columns do).
-    __device__ inline void run(const Segment& s, uint32_t i, uint32_t step, int wave)
+    // Asks for the queries and the first tile of a segment, of which the wave is to take tiles i, i + step, ..
+    __device__ inline void begin(const Segment& s, uint32_t i, uint32_t step, int wave)
     {
-#pragma unroll
-        for (int d = 0; d < D / 16; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-        sum = 0.f;
-        ref = -3e38f;
         bad = s.vis.length < 0;
         if constexpr (QLDS) {
             if (s.count > 0) {
@@ -352,15 +351,30 @@ template <int P, int D, bool MASK> struct Attn {
             }
             lds_barrier();
         }
-        if (i < s.count) {
-            Tile t = look_up(s, i), next = look_up(s, i + step);
-            if constexpr (!QLDS) {
-                const char* row = query_row(s);
+        if constexpr (!QLDS) if (i < s.count) {
+            const char* row = query_row(s);
 #pragma unroll
-                for (int x = 0; x < NQ; ++x) q[x] = query_piece(row, x);
-            }
-            request_keys(s, t);
-            request_values(s, t);
+            for (int x = 0; x < NQ; ++x) q[x] = query_piece(row, x);
+            request_first(s, i, step);
+        }
+    }
+    __device__ inline void request_first(const Segment& s, uint32_t i, uint32_t step)
+    {
+        t = look_up(s, i);
+        next = look_up(s, i + step);
+        request_keys(s, t);
+        request_values(s, t);
+    }
+
+    // Takes them; afterwards columns 0 .. 7 hold the heads' results (fp32: all columns do).
+    __device__ inline void run(const Segment& s, uint32_t i, uint32_t step)
+    {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        sum = 0.f;
+        ref = -3e38f;
+        if (i < s.count) {
+            if constexpr (QLDS) request_first(s, i, step);
             f32x4 x[NT];
             for (; i + step < s.count; i += step) {
                 const i32x4 exps = ke;
@@ -520,20 +534,14 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
     };
     // Every wave looks at the lengths of all sequences, `per` consecutive ones to a lane.
     const int per = (a.batch + 63) / 64;
-    int one = 0;                           // the lane's length, where each has one
-    uint32_t mine = 0;
-    int longest = 0;
+    int one = 0, longest = 0;              // the lane's length and its tiles, where each has one; the most tiles of a pair
     if (per == 1) {
         one = a.length[min(lane, a.batch - 1)];
         longest = tiles_in(visible_in(one)).count;
-        mine = lane < a.batch ? units_of(longest) : 0;
     } else {
-        for (int i = lane * per; i < min((lane + 1) * per, a.batch); ++i) {
-            const int n = tiles_in(visible_in(a.length[i])).count;
-            longest = max(longest, n);
-            mine += units_of(n);
-        }
+        for (int i = lane * per; i < min((lane + 1) * per, a.batch); ++i) longest = max(longest, tiles_in(visible_in(a.length[i])).count);
     }
+    const int own = longest;
     longest = __builtin_amdgcn_readlane(scan(longest, [](int x, int y) { return max(x, y); }), 63);
     auto segment = [&](int b, int h) {
         Segment s;
@@ -548,10 +556,12 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
     A w(a, queries);
 
     // Pairs of a few tiles: a wave to each, which needs nobody else.
-    if (!A::QLDS && longest <= kSoloTiles) {
-        for (uint32_t pair = wave * gridDim.x + blockIdx.x; pair < (uint32_t)a.batch * H; pair += gridDim.x * NW) {   // over all compute units first
+    const uint32_t pairs = (uint32_t)a.batch * H;
+    if (!A::QLDS && longest <= (pairs > 2 * a.blocks ? 2 : 1) * F::SOLO) {
+        for (uint32_t pair = wave * a.blocks + blockIdx.x; pair < pairs; pair += a.blocks * NW) {   // over all compute units first
             const Segment s = segment(pair / H, pair % H);
-            w.run(s, 0, 1, wave);
+            w.begin(s, 0, 1, wave);
+            w.run(s, 0, 1);
             LateArgs l = late_args();
             const int G = l->G;
             if (w.m < G) {
@@ -571,30 +581,67 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
         return;
     }
 
-    const bool split = longest > kWholeTiles;
-    if (!split) mine = max(0, min(per, a.batch - lane * per));
-    const uint32_t upto = scan(mine, [](int x, int y) { return x + y; });
-    const uint32_t total = __builtin_amdgcn_readlane(upto, 63) * (uint32_t)H, share = units_per_block(total, gridDim.x);
+    // The unit, in tiles: a pair, where the longest is short; else what gives every block one unit, where the pairs are few (a
+    // block with parts of two pairs pays for both), else the least.
+    uint32_t unit = kUnitTiles, upto, total;
+    auto add = [&](uint32_t n) { upto = scan(n, [](int x, int y) { return x + y; }); total = __builtin_amdgcn_readlane(upto, 63) * (uint32_t)H; return n; };
+    auto units_in_lane = [&]() {
+        if (per == 1) return lane < a.batch ? units_of(own, unit) : 0u;
+        uint32_t n = 0;
+        for (int i = lane * per; i < min((lane + 1) * per, a.batch); ++i) n += units_of(tiles_in(visible_in(a.length[i])).count, unit);
+        return n;
+    };
+    if ((uint32_t)longest <= whole_tiles(F::TILE * D * F::EB * 2, pairs, a.blocks)) unit = max(longest, 1);
+    uint32_t mine = add(units_in_lane());
+    if (per == 1 && 2 * pairs <= a.blocks && total > a.blocks) {
+        unit *= units_per_block(total, a.blocks);
+        unit = (unit + NW - 1) / NW * NW;              // (a round of a tile for each wave takes as long if some have none)
+        for (const uint32_t more = max(unit / 64 * NW, (uint32_t)NW);; unit += more) {
+            mine = add(units_in_lane());
+            if (total <= a.blocks) break;
+        }
+    }
+    const uint32_t share = units_per_block(total, a.blocks);
     uint32_t cur = share * blockIdx.x;
     if (cur >= total) return;
     const uint32_t end = min(cur + share, total);
     const int owner = __ffsll((unsigned long long)__ballot(cur < upto * H)) - 1;
     uint32_t off = cur - __builtin_amdgcn_readlane(upto - mine, owner) * H;   // units between the start of sequence b and the block's first
     int b = owner * per;
-    auto units = [&](const Segment& s) { return split ? units_of(s.tiles.count) : 1u; };
+    auto units = [&](const Segment& s) { return units_of(s.tiles.count, unit); };
     if (per > 1)
         for (uint32_t n; off >= (n = units(segment(b, 0)) * H); ++b) off -= n;
 
-    while (true) {
-        Segment s = segment(b, 0);
-        const uint32_t n = units(s);
+    // the block's share of the pair that `off` lies in: `here` units from the pair's unit `first` of n on
+    Segment s;
+    uint32_t n, first, here;
+    auto place = [&]() {
+        s = segment(b, 0);
+        n = units(s);
         s.h = off / n;
-        const uint32_t first = off - s.h * n, here = min(n - first, end - cur);
-        if (split && s.count > 0) {
-            s.first = first * kUnitTiles;
-            s.count = min(here * kUnitTiles, s.tiles.count - s.first);
+        first = off - s.h * n;
+        here = min(n - first, end - cur);
+        if (s.count > 0) {
+            s.first = first * unit;
+            s.count = min(here * unit, s.tiles.count - s.first);
         }
-        w.run(s, wave, NW, wave);
+    };
+    place();
+    w.begin(s, wave, NW, wave);
+    while (true) {
+        w.run(s, wave, NW);
+        const bool alone = here == n, any = s.tiles.count > 0;
+        const uint32_t at = cur - first, of = n;       // the pair's units
+        const int64_t pair = (int64_t)b * H + s.h;
+        const int slot = 2 * (int)blockIdx.x + (first == 0 ? 1 : 0);
+        cur += here;
+        off += here;
+        if (off == n * H) { off = 0; ++b; }
+        const bool more = cur < end;
+        if (more) {                                    // the next pair's first rows are under way while this one's results are joined
+            place();
+            if constexpr (!A::QLDS) w.begin(s, wave, NW, wave);
+        }
         LateArgs l = late_args();
         const int G = l->G;
         if (w.m < G) {
@@ -604,9 +651,6 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
         }
         lds_barrier();
 
-        const bool alone = here == n, any = s.tiles.count > 0;
-        const int64_t unit = (int64_t)b * H + s.h;
-        const int slot = 2 * (int)blockIdx.x + (first == 0 ? 1 : 0);
         for (int i = tid; i < G * D; i += kThreads) {
             const int g = i / D, d = i - g * D;
             float ref = stat[0][g].x, sum = 0.f, o = 0.f;
@@ -619,29 +663,28 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
                 o = fmaf(by, acc[x][g][d], o);
             }
             if (alone) {
-                l->out[unit * G * D + i] = any ? o / sum : sum;                  // nothing visible: 0, or NaN
-                if (d == 0 && l->lse) l->lse[unit * G + g] = any ? (ref + log2f(sum)) * 0.6931471805599453f : sum - INFINITY;
+                l->out[pair * G * D + i] = any ? o / sum : sum;                  // nothing visible: 0, or NaN
+                if (d == 0 && l->lse) l->lse[pair * G + g] = any ? (ref + log2f(sum)) * 0.6931471805599453f : sum - INFINITY;
             } else {
                 publish(l->part_o + (int64_t)slot * G * D + i, o);
                 if (d == 0) { publish(l->part_ml + ((int64_t)slot * G + g) * 2, ref); publish(l->part_ml + ((int64_t)slot * G + g) * 2 + 1, sum); }
             }
         }
-        if (!alone) join_parts<D>(parts_of(cur - first, n, share), slot, unit, stat, acc, &arrived);
-        cur += here;
-        if (cur >= end) break;
-        off += here;
-        if (off == n * H) { off = 0; ++b; }
+        if (!alone) join_parts<D>(parts_of(at, of, share), slot, pair, stat, acc, &arrived);
+        if (!more) break;
         lds_barrier();                                 // the next pair's results go to the same LDS
+        if constexpr (A::QLDS) w.begin(s, wave, NW, wave);
     }
 }
 
-template <int P, int D> hipError_t launch(const PagedAttnArgs& a, int compute_units, hipStream_t st)
+template <int P, int D> hipError_t launch(PagedAttnArgs a, int compute_units, hipStream_t st)
 {
     int64_t grid = compute_units < kPagedMaxBlocks ? compute_units : kPagedMaxBlocks;
     // no more blocks than could have units
     constexpr int unit = Form<P>::TILE * kUnitTiles;
     const int64_t units = (int64_t)a.batch * a.pages.heads * (((int64_t)a.pages.cols * a.pages.rows + unit - 1) / unit);
     if (grid > units) grid = units;
+    a.blocks = (uint32_t)grid;
     if (a.window > 0) hipLaunchKernelGGL((paged_attn_kernel<P, D, true>), dim3((unsigned)grid), dim3(kThreads), 0, st, a);
     else hipLaunchKernelGGL((paged_attn_kernel<P, D, false>), dim3((unsigned)grid), dim3(kThreads), 0, st, a);
     return hipGetLastError();

@@ -76,13 +76,21 @@ __host__ __device__ inline Tiles tiles_of(const Visible& v, int32_t tile)
     return Tiles{low, high, low + end - high};
 }
 
-// A decode step's work is cut into units of one (sequence, head) pair: kUnitTiles tiles, or the whole pair where no pair of the
-// step has more than kWholeTiles.  The units of all pairs are numbered through, `share` consecutive ones to a block.  A pair of n
-// units from number `begin` on is worked on by `parts` blocks from `from` on; each but the one with the pair's first unit leaves
-// its partial result in its slot 0, that one in slot 1, so a block that ends one pair and begins another needs two.
-constexpr int kUnitTiles = 4, kWholeTiles = 16;
-__host__ __device__ inline uint32_t units_of(int32_t tiles) { return tiles > 0 ? ((uint32_t)tiles + kUnitTiles - 1) / kUnitTiles : 1; }   // somebody has to write an empty pair's output
+// A decode step's work is cut into units of `unit` tiles of one (sequence, head) pair.  The units of all pairs are numbered
+// through, `share` consecutive ones to a block.  A pair of n units from number `begin` on is worked on by `parts` blocks from
+// `from` on; each but the one with the pair's first unit leaves its partial result in its slot 0, that one in slot 1, so a block
+// that ends one pair and begins another needs two.
+constexpr int kUnitTiles = 4;              // the least
+__host__ __device__ inline uint32_t units_of(int32_t tiles, uint32_t unit) { return tiles > 0 ? ((uint32_t)tiles + unit - 1) / unit : 1; }   // somebody has to write an empty pair's output
 __host__ __device__ inline uint32_t units_per_block(uint32_t total, uint32_t blocks) { return (total + blocks - 1) / blocks; }
+// Up to how many tiles a pair is left whole.  Reading 128 KB takes a compute unit about as long as it takes to publish partial
+// results and to add them up; with as many pairs as blocks four times that, because cutting pairs then leaves most blocks with
+// parts of two (bf16, 4 heads of 128, tiles of 16 KB: 64 pairs of 13 tiles whole 10.1 us, cut 8.8; 256 of 10 to 19 tiles 13.6 / 17.5).
+__host__ __device__ inline uint32_t whole_tiles(uint32_t tile_bytes, uint32_t pairs, uint32_t blocks)
+{
+    const uint32_t times = 4 * pairs / blocks;
+    return 131072 / tile_bytes * (times < 1 ? 1 : times > 4 ? 4 : times);
+}
 struct Parts {
     int from, parts;
     __host__ __device__ inline int slot(int i) const { return 2 * (from + i) + (i == 0 ? 1 : 0); }
@@ -138,6 +146,7 @@ struct PagedAttnArgs {
     int32_t sink, window;
     float scale_log2;
     uint32_t page_bytes;                   // of one page of K, or of V: under 4 GiB
+    uint32_t blocks;                       // the grid (set by the launch)
 };
 
 hipError_t launch_rotate(int dtype, int page_dtype, const RotateArgs& a, int batch, hipStream_t st);

@@ -120,7 +120,7 @@ int main()
     check_share({0}, 1, 1);
     check_share({1 << 22}, 1, kPagedMaxBlocks);
     check_share(std::vector<int>(511, 1 << 22), 1, kPagedMaxBlocks);         // 2^31 - 2^22 units
-    CHECK(units_of(0) == 1 && units_of(1) == 1 && units_of(4) == 1 && units_of(5) == 2);
+    CHECK(units_of(0, 4) == 1 && units_of(1, 4) == 1 && units_of(4, 4) == 1 && units_of(5, 4) == 2 && units_of(1 << 24, 1) == 1 << 24);
     CHECK(units_countable(511, 1, 1 << 20, 256) && !units_countable(512, 1, 1 << 20, 256) && !units_countable(65535, 65535, 1, 16));
 
     // rows of a call: spans, and the tiles of 16 positions that cover them
