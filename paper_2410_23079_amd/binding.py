@@ -355,13 +355,17 @@ class Rotary:
         self.c = _Rotary(_ptr(q_weight), _ptr(k_weight), _ptr(inv_freq), eps, 0 if inv_freq is None else 2 * inv_freq.numel(),
                          int(interleaved), 0)
         self.ref = ctypes.addressof(self.c)
+        weights = [t for t in (q_weight, k_weight) if t is not None]
+        if len({(t.dtype, t.shape[0]) for t in weights}) > 1 or len({t.device for t in weights + ([] if inv_freq is None else [inv_freq])}) > 1:
+            raise BuzzError(-1, "Rotary", "weights of one length and type, all on one device")
+        # what rows must be like: anything where nothing says so
+        self.dtype, self.dim = (weights[0].dtype, weights[0].shape[0]) if weights else (None, None)
+        self.at = weights[0].get_device() if weights else None if inv_freq is None else inv_freq.get_device()
 
     def check(self, dtype, head_dim, index):
-        for t in (self.q_weight, self.k_weight):
-            if t is not None and (t.dtype is not dtype or t.shape[0] != head_dim or t.get_device() != index):
-                _wrong("Rotary", t, f"wanted [{head_dim}] {dtype} on device {index}")
-        if self.inv_freq is not None and self.inv_freq.get_device() != index:
-            _wrong("Rotary inv_freq", self.inv_freq, f"wanted it on device {index}")
+        if (self.dtype is not dtype and self.dtype is not None) or (self.dim != head_dim and self.dim is not None) or \
+                (self.at != index and self.at is not None):
+            raise BuzzError(-1, "Rotary", f"made for rows of {self.dim} {self.dtype} on device {self.at}, not {head_dim} {dtype} on {index}")
         return self.ref
 
 

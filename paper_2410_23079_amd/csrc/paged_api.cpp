@@ -10,7 +10,6 @@ using namespace buzz;
 namespace {
 
 constexpr uint32_t kPagedMagic = 0xB0220CA6u;
-constexpr int64_t kMaxRows = (int64_t)1 << 27;         // rows of a sequence in one call: a grid has fewer than 2^32 threads in x
 constexpr int64_t kMaxTokens = (int64_t)1 << 28;       // tokens of a sequence in a cache
 
 size_t align_up(size_t x) { return (x + 255) / 256 * 256; }
@@ -112,7 +111,7 @@ int check_call(const buzz_paged_t* c, int32_t batch, int64_t n_rows, const int32
     if (!alive(c) || batch < 0 || n_rows < 0) return BUZZ_EINVAL;
     if (!c->dry && batch > 0 && n_rows > 0 && !table) return BUZZ_EINVAL;
     if (batch > c->cfg.batch || n_rows > (int64_t)c->cfg.table_cols * c->cfg.page_rows) return BUZZ_ECAPACITY;
-    return n_rows > kMaxRows ? BUZZ_EUNSUPPORTED : BUZZ_OK;
+    return rows_launchable(n_rows, (int64_t)c->cfg.n_q_heads + 2 * (int64_t)c->cfg.n_kv_heads) ? BUZZ_OK : BUZZ_EUNSUPPORTED;
 }
 
 }  // namespace
@@ -126,7 +125,7 @@ int buzz_qk_norm_rotate(int32_t dtype, int32_t head_dim, int32_t n_q_heads, int3
     if (dtype < BUZZ_FP32 || dtype > BUZZ_BF16 || head_dim < 1 || batch < 0 || n_rows < 0 || !rotary) return BUZZ_EINVAL;
     if ((q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr)) return BUZZ_EINVAL;
     if ((q && n_q_heads < 1) || (k && n_kv_heads < 1)) return BUZZ_EINVAL;
-    if (!head_dim_ok(head_dim) || batch > 65535 || n_rows > kMaxRows || (q && n_q_heads > 65535) || (k && n_kv_heads > 65535)) return BUZZ_EUNSUPPORTED;
+    if (!head_dim_ok(head_dim) || batch > 65535 || !rows_launchable(n_rows, (q ? (int64_t)n_q_heads : 0) + (k ? (int64_t)n_kv_heads : 0))) return BUZZ_EUNSUPPORTED;
     RotateArgs a{};
     if (int rc = take_rotary(rotary, head_dim, &a)) return rc;
     if (batch == 0 || n_rows == 0) return BUZZ_OK;

@@ -13,9 +13,9 @@
 //   - these, as weights, are one operand of the second product as they stand; its other operand is 16 bytes of one
 //     column of V for the same KG keys, which is why the pages hold V that way.  No LDS, no transposition, no lane
 //     crossing between the two products.
-//   - Weights keep more than 16 bits: with 16-bit operands columns 0..7 carry the weights rounded to the operand's
-//     type, columns 8..15 (the same heads again) what that rounding left over.  The unused half of the matrix
-//     instruction does it for free; the sum of both halves has at least 16 bits.
+//   - Weights keep 22 bits or more: with 16-bit operands columns 0..7 carry the weights rounded to the operand's type,
+//     columns 8..15 (the same heads again) what that rounding left over, and in bf16 another product what is left then.
+//     The unused half of the matrix instruction does most of it for free.
 //
 // Layout of the work.  Sequences differ in length, and their lengths are known on the device only.  So the tiles of
 // all (sequence, head) pairs, 4 KG keys each, are numbered through, and each block takes the same number of
@@ -85,17 +85,22 @@ template <bool F16> __device__ inline i32x4 widen(i32x4 x, int at)
     return r;
 }
 
-// Two weights as one dword of the second product's operand: rounded to its type, or (left = 1) what that left over.
-template <bool F16> __device__ inline int pack(float x, float y, float left)
+// Two weights as dwords of the second product's operands.  With f16, columns 0 .. 7 take them rounded (left 0), columns 8 .. 15
+// what that rounding left over (left 1): 22 bits together.  bf16 has 8 bits, so what the second rounding leaves over goes into an
+// operand of its own, columns 0 .. 7 (the others 0): 24 bits.
+struct Packed { int both, rest; };
+template <bool F16> __device__ inline Packed pack(float x, float y, float left)
 {
     if constexpr (F16) {
         const f16x2_t h = {(_Float16)x, (_Float16)y};
         const f16x2_t r = {(_Float16)fmaf(-left, (float)h[0], x), (_Float16)fmaf(-left, (float)h[1], y)};
-        return __builtin_bit_cast(int, r);
+        return Packed{__builtin_bit_cast(int, r), 0};
     } else {
         const bf16x2_t h = {(__bf16)x, (__bf16)y};
-        const bf16x2_t r = {(__bf16)fmaf(-left, (float)h[0], x), (__bf16)fmaf(-left, (float)h[1], y)};
-        return __builtin_bit_cast(int, r);
+        const float x1 = x - (float)h[0], y1 = y - (float)h[1];
+        const bf16x2_t r = {(__bf16)x1, (__bf16)y1};
+        const bf16x2_t e = {(__bf16)(x1 - (float)r[0]), (__bf16)(y1 - (float)r[1])};
+        return Packed{__builtin_bit_cast(int, left == 0.f ? h : r), left == 0.f ? __builtin_bit_cast(int, e) : 0};
     }
 }
 
@@ -328,12 +333,18 @@ template <int P, int D, bool MASK> struct Attn {
             }
 #pragma unroll
             for (int hf = 0; hf < NT / 2; ++hf) {
-                const i32x4 p = {pack<F::F16V>(s[2 * hf][0], s[2 * hf][1], left), pack<F::F16V>(s[2 * hf][2], s[2 * hf][3], left),
-                                 pack<F::F16V>(s[2 * hf + 1][0], s[2 * hf + 1][1], left), pack<F::F16V>(s[2 * hf + 1][2], s[2 * hf + 1][3], left)};
+                i32x4 p, rest;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const Packed x = pack<F::F16V>(s[2 * hf + i / 2][i % 2 * 2], s[2 * hf + i / 2][i % 2 * 2 + 1], left);
+                    p[i] = x.both;
+                    rest[i] = x.rest;
+                }
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) {
-                    if constexpr (F::E4M3) o[d] = mma<false>(widen<false>(vv[d], hf), p, o[d]);
-                    else o[d] = mma<F::F16V>(vv[d], p, o[d]);
+                    const i32x4 v = F::E4M3 ? widen<false>(vv[d], hf) : vv[d];
+                    o[d] = mma<F::F16V>(v, p, o[d]);
+                    if constexpr (!F::F16V) o[d] = mma<false>(v, rest, o[d]);
                     if constexpr (D == 256 && F::E4M3) if (d % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -534,12 +545,23 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
     };
     // Every wave looks at the lengths of all sequences, `per` consecutive ones to a lane.
     const int per = (a.batch + 63) / 64;
+    auto for_lengths = [&](auto f) {       // of the lane, eight asked for at a time
+        const int to = min((lane + 1) * per, a.batch);
+        for (int i = lane * per; i < to; i += 8) {
+            int n[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) n[j] = a.length[min(i + j, to - 1)];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i + j < to) f(n[j]);
+        }
+    };
     int one = 0, longest = 0;              // the lane's length and its tiles, where each has one; the most tiles of a pair
     if (per == 1) {
         one = a.length[min(lane, a.batch - 1)];
         longest = tiles_in(visible_in(one)).count;
     } else {
-        for (int i = lane * per; i < min((lane + 1) * per, a.batch); ++i) longest = max(longest, tiles_in(visible_in(a.length[i])).count);
+        for_lengths([&](int n) { longest = max(longest, tiles_in(visible_in(n)).count); });
     }
     const int own = longest;
     longest = __builtin_amdgcn_readlane(scan(longest, [](int x, int y) { return max(x, y); }), 63);
@@ -587,9 +609,9 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
     auto add = [&](uint32_t n) { upto = scan(n, [](int x, int y) { return x + y; }); total = __builtin_amdgcn_readlane(upto, 63) * (uint32_t)H; return n; };
     auto units_in_lane = [&]() {
         if (per == 1) return lane < a.batch ? units_of(own, unit) : 0u;
-        uint32_t n = 0;
-        for (int i = lane * per; i < min((lane + 1) * per, a.batch); ++i) n += units_of(tiles_in(visible_in(a.length[i])).count, unit);
-        return n;
+        uint32_t sum = 0;
+        for_lengths([&](int n) { sum += units_of(tiles_in(visible_in(n)).count, unit); });
+        return sum;
     };
     if ((uint32_t)longest <= whole_tiles(F::TILE * D * F::EB * 2, pairs, a.blocks)) unit = max(longest, 1);
     uint32_t mine = add(units_in_lane());

@@ -46,6 +46,8 @@ __host__ __device__ inline Span row_span(const int32_t* start, const int32_t* co
 
 // Tiles of 16 positions that n rows can touch, wherever the first one stands.
 __host__ __device__ inline int64_t tiles_of_rows(int64_t n) { return n <= 0 ? 0 : (n + 14) / kPagedTileTokens + 1; }
+// Whether a grid has room for them: fewer than 2^32 threads, 256 for a tile and head at most.
+inline bool rows_launchable(int64_t n, int64_t heads) { return heads <= 65535 && n <= 1 << 28 && tiles_of_rows(n) * heads <= UINT32_MAX / 256; }
 
 // Keys that the new token of a sequence of `length` tokens attends to: [0, sink_end) and [from, length).
 struct Visible {
@@ -88,8 +90,8 @@ __host__ __device__ inline uint32_t units_per_block(uint32_t total, uint32_t blo
 // parts of two (bf16, 4 heads of 128, tiles of 16 KB: 64 pairs of 13 tiles whole 10.1 us, cut 8.8; 256 of 10 to 19 tiles 13.6 / 17.5).
 __host__ __device__ inline uint32_t whole_tiles(uint32_t tile_bytes, uint32_t pairs, uint32_t blocks)
 {
-    const uint32_t times = 4 * pairs / blocks;
-    return 131072 / tile_bytes * (times < 1 ? 1 : times > 4 ? 4 : times);
+    const uint32_t times = pairs >= blocks ? 4 : 4 * pairs / blocks;
+    return 131072 / tile_bytes * (times < 1 ? 1 : times);
 }
 struct Parts {
     int from, parts;
@@ -120,7 +122,7 @@ struct RotateArgs {
     int32_t half;                          // rot_dim / 2
     int32_t interleaved;
     int32_t Hq, Hkv, D;
-    int32_t q_chunk, kv_chunk, q_jobs, k_jobs, v_jobs;   // heads per block; blocks (grid's y) per tile of positions (set by the launch)
+    int32_t q_chunk, kv_chunk, v_chunk, q_jobs, k_jobs, v_jobs;   // heads per block; blocks per tile of positions (set by the launch)
     PageArgs pages;                        // k NULL: dense
 };
 
@@ -129,7 +131,7 @@ struct ReadArgs {
     const int32_t* start; const int32_t* count;
     int64_t n_rows;
     PageArgs pages;
-    int32_t chunk, k_jobs, v_jobs;         // set by the launch
+    int32_t chunk, k_jobs, v_jobs;         // likewise
 };
 
 struct PagedAttnArgs {

@@ -6,8 +6,8 @@ Tolerances count roundings.  u = 2^-24 is half a step of fp32; a result in type 
                     of |x| + |y| of the pair after the norm
   8-bit rows        half a step of e4m3 (2^-4 of the value's power of two, at least 2^-10 of the row's) on top of the above
   decode            logits: D products summed in at most D + 8 steps, (D + 8) u of scale * sum |q_i k_i|, twice (numerator and
-                    sum), and 2 u of the logit for its product with log2 e; exp2 2 u; weights of 16 bits 2^-17; sums over
-                    N keys in at most N / 16 + 64 steps.  All of it of sum_j p_j |v_j|
+                    sum), and 2 u of the logit for its product with log2 e; exp2 2 u; weights of 22 bits (2^-23, twice); sums
+                    over N keys in at most N / 16 + 64 steps.  All of it of sum_j p_j |v_j|
 """
 import math
 
@@ -317,7 +317,7 @@ def attention(cache, q, table, lengths, scale=None):
         ds = (D + 8) * U * scale * torch.matmul(qb.abs(), kb.abs().nan_to_num(posinf=0.0).transpose(1, 2)) + 2 * U * s.abs().nan_to_num(posinf=0.0, neginf=0.0)
         ds = torch.where(p > 0, ds, 0.0).amax(-1, keepdim=True)
         sums = (len(js) / 16 + 64) * U
-        tol_o[b] = ((2 * ds + 2.0 ** -17 + sums + 4 * U) * torch.matmul(p, vb.abs()) / total).view(-1, D)
+        tol_o[b] = ((2 * ds + 2.0 ** -22 + sums + 4 * U) * torch.matmul(p, vb.abs()) / total).view(-1, D)
         tol_l[b] = (ds + sums + 4 * U + 4 * U * (top + total.log()).abs()).flatten()
     return out, lse, tol_o, tol_l
 
@@ -375,6 +375,20 @@ def test_decode_of_many_sequences(dtype, page_dtype):
     lengths = [int(x) for x in np.random.RandomState(1).randint(0, 90, size=391)]
     c, table, q = filled(6, lengths, 3, 2, 64, dtype, page_dtype, 32)
     check_decode(c, table, q, lengths, f"many {dtype} {page_dtype}")
+
+
+@pytest.mark.parametrize("B,H,G,D,dtype,page_dtype,longest,mask", [
+    (70, 40, 1, 64, "bf16", None, 60, {}),                     # more pairs than waves, each a wave's; two lengths to a lane
+    (64, 8, 2, 128, "fp16", None, 480, {}),                    # whole pairs, two to a block
+    (40, 8, 1, 64, "bf16", "e4m3", 2500, {}),                  # blocks with parts of several pairs
+    (33, 8, 3, 256, "bf16", None, 900, {}), (20, 8, 2, 128, "fp32", None, 1500, {}), (66, 4, 5, 256, "fp16", "e4m3", 400, {}),
+    (48, 4, 8, 128, "fp16", "e4m3", 3000, dict(sink=100, window=1000)), (90, 3, 4, 128, "bf16", None, 1300, dict(sink=7, window=300)),
+    (2, 60, 1, 128, "bf16", None, 5000, {}), (3, 30, 2, 64, "fp16", None, 9000, {})])   # few pairs: a unit to every block
+def test_shares_of_blocks(B, H, G, D, dtype, page_dtype, longest, mask):
+    lengths = [int(x) for x in np.random.RandomState(B + H).randint(0, longest + 1, size=B)]
+    lengths[B // 2] = longest
+    c, table, q = filled(B * 100 + H, lengths, H, G, D, dtype, page_dtype, 64, **mask)
+    check_decode(c, table, q, lengths, f"shares {B} {H} {D} {dtype} {page_dtype} {longest}")
 
 
 @pytest.mark.parametrize("dtype,page_dtype", PAGES)
@@ -507,7 +521,7 @@ def test_offsets_beyond_32_bits():
     c.decode(q, ints(table), ints([700]), out)
     p = torch.softmax(torch.matmul(k[0].double(), q[0].double()[..., None])[..., 0] / 16, -1)
     want = (p[..., None] * v[0].double()).sum(1)
-    assert_within(out[0], want, (2 * 264 * U * 64 + 2.0 ** -17 + 108 * U) * (p[..., None] * v[0].double().abs()).sum(1))
+    assert_within(out[0], want, (2 * 264 * U * 64 + 2.0 ** -22 + 108 * U) * (p[..., None] * v[0].double().abs()).sum(1))
 
 
 # ------------------------------------------------------------------------------------------------ all of them together

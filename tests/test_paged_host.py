@@ -154,3 +154,94 @@ def test_the_binding_looks_at_tensors_before_their_addresses_are_used():
         with pytest.raises(BuzzError) as e:
             call()
         assert e.value.code == -1, i
+
+
+# ------------------------------------------------------------------------------------------------ what is enqueued
+@pytest.fixture(scope="module")
+def recorded(tmp_path_factory):
+    """The library's objects linked against a recorder that takes kernel launches in place of the HIP runtime."""
+    if shutil.which("hipcc") is None:
+        pytest.skip("hipcc not on PATH")
+    from paper_2410_23079_amd.build import CSRC, SOURCES, build
+    objs = [os.path.join(CSRC, stem + ".o") for _, stem, _ in SOURCES]
+    if not all(os.path.exists(o) for o in objs):
+        build()
+    tmp = tmp_path_factory.mktemp("recorder")
+    rec, so = str(tmp / "launch_recorder.o"), str(tmp / "libbuzz_recorded.so")
+    subprocess.run(["hipcc", "-x", "hip", "--cuda-host-only", "-std=c++17", "-O1", "-fPIC", "-I", os.path.join(ROOT, "include"),
+                    "-I", CSRC, "-c", os.path.join(HERE, "launch_recorder.cpp"), "-o", rec], check=True, capture_output=True)
+    subprocess.run(["g++", "-shared", "-Wl,-Bsymbolic", "-Wl,--no-undefined", "-o", so, rec, *objs], check=True, capture_output=True)
+    lib, real = ctypes.CDLL(so), load_library()
+    for name in ("buzz_qk_norm_rotate", "buzz_paged_create", "buzz_paged_destroy", "buzz_paged_append", "buzz_paged_read", "buzz_paged_decode"):
+        getattr(lib, name).argtypes = getattr(real, name).argtypes
+    lib.rec_kernel.restype = ctypes.c_char_p
+    lib.rec_value.restype = ctypes.c_longlong
+    lib.rec_value.argtypes = [ctypes.c_int, ctypes.c_char_p]
+    return lib
+
+
+def made(lib, **kw):
+    c, h = cfg(**kw), ctypes.c_void_p()
+    exps = (0x300000, 0x400000) if c.page_dtype else (None, None)
+    lib.rec_reset(-1)
+    assert lib.buzz_paged_create(c.to_c(), _Pages(0x100000, 0x200000, *exps), 0x500000, 1 << 40, None, ctypes.byref(h)) == 0
+    assert lib.rec_count() == 1 and b"clear" in lib.rec_kernel(0)          # the counters, by a kernel
+    lib.rec_reset(-1)
+    return h
+
+
+def test_every_call_is_one_launch_and_a_launch_that_fails_is_told(recorded):
+    lib, r, rot = recorded, rows(), _Rotary(None, None, 0x1000, 1e-6, 64, 0, 0)
+    h = made(lib)
+    calls = [lambda: lib.buzz_paged_append(h, ctypes.byref(rot), r, r, r, r, 3, 40, 0x1000, 0x1000, None, None),
+             lambda: lib.buzz_paged_read(h, r, r, 3, 40, 0x1000, None, None, None),
+             lambda: lib.buzz_paged_decode(h, r, 3, 0x1000, 0x1000, 0x1000, None, None),
+             lambda: lib.buzz_qk_norm_rotate(2, 128, 8, 2, ctypes.byref(rot), r, r, r, r, 3, 40, None, None, None)]
+    for call in calls:
+        lib.rec_reset(-1)
+        assert call() == 0 and lib.rec_count() == 1
+        lib.rec_reset(0)
+        assert call() == -4
+    lib.rec_reset(-1)
+    assert lib.buzz_paged_append(h, None, None, r, r, None, 0, 40, 0x1000, None, None, None) == 0
+    assert lib.buzz_paged_append(h, None, None, r, r, None, 3, 0, 0x1000, None, None, None) == 0
+    assert lib.buzz_paged_read(h, None, None, 3, 40, 0x1000, None, None, None) == 0
+    assert lib.buzz_paged_decode(h, r, 0, 0x1000, 0x1000, 0x1000, None, None) == 0
+    assert lib.rec_count() == 0                                            # nothing to do
+    assert lib.buzz_paged_append(h, None, None, r, None, None, 3, 40, 0x1000, None, None, None) == -1
+    assert lib.buzz_paged_append(h, None, None, r, r, None, 3, 40, None, None, None, None) == -1
+    assert lib.buzz_paged_decode(h, rows(ptr=0x1008), 3, 0x1000, 0x1000, 0x1000, None, None) == -5
+    assert lib.buzz_paged_decode(h, r, 3, 0x1000, 0x1000, 0x1004, None, None) == -5
+    assert lib.buzz_paged_decode(h, r, 3, 0x1000, None, 0x1000, None, None) == -1
+    assert lib.rec_count() == 0
+    assert lib.buzz_paged_destroy(h) == 0
+    c, x = cfg(), ctypes.c_void_p()
+    lib.rec_reset(0)
+    assert lib.buzz_paged_create(c.to_c(), _Pages(0x1000, 0x2000, None, None), 0x1000, 1 << 40, None, ctypes.byref(x)) == -4
+    assert x.value is None
+    lib.rec_reset(-1)
+
+
+@pytest.mark.parametrize("kw,batch,most", [
+    (dict(batch=1, n_q_heads=1, n_kv_heads=1, table_cols=1), 1, 1), (dict(table_cols=64), 3, 2 * 3 * 64 // 4),
+    (dict(batch=64, table_cols=4096), 64, 512), (dict(batch=4, page_dtype="e4m3", table_cols=64), 4, 512),
+    (dict(dtype="fp32", table_cols=2), 3, 6)])
+def test_the_decode_grid_has_no_more_blocks_than_there_can_be_work(recorded, kw, batch, most):
+    h = made(recorded, **kw)
+    assert recorded.buzz_paged_decode(h, rows(), batch, 0x1000, 0x1000, 0x1000, None, None) == 0
+    assert 1 <= recorded.rec_value(0, b"grid_x") <= most and recorded.rec_value(0, b"grid_y") == recorded.rec_value(0, b"grid_z") == 1
+    assert recorded.rec_value(0, b"block_x") == 512
+    recorded.buzz_paged_destroy(h)
+
+
+@pytest.mark.parametrize("n,batch,D,dtype", [(1, 3, 128, "bf16"), (17, 2, 64, "fp32"), (300, 1, 256, "fp16"), (20000, 3, 128, "bf16"), (2, 1, 128, "fp32")])
+def test_the_row_grids_cover_every_tile_of_every_sequence(recorded, n, batch, D, dtype):
+    """16 positions to a tile, wherever the first row stands; as many blocks per tile as jobs."""
+    h, r, rot = made(recorded, head_dim=D, dtype=dtype, table_cols=1000, page_rows=32), rows(), _Rotary(None, None, 0x1000, 1e-6, 64, 0, 0)
+    assert recorded.buzz_paged_append(h, ctypes.byref(rot), r, r, r, r, batch, n, 0x1000, 0x1000, None, None) == 0
+    assert recorded.buzz_paged_read(h, r, r, batch, n, 0x1000, 0x1000, None, None) == 0
+    assert recorded.buzz_paged_read(h, r, None, batch, n, 0x1000, 0x1000, None, None) == 0
+    for i, least in ((0, 3), (1, 2), (2, 1)):                              # q, k and v; k and v; k: a job each at least
+        assert recorded.rec_value(i, b"grid_x") == (n + 14) // 16 + 1 and recorded.rec_value(i, b"grid_z") == batch
+        assert least <= recorded.rec_value(i, b"grid_y") <= 8 + 2 + 2
+    recorded.buzz_paged_destroy(h)
