@@ -256,11 +256,11 @@ int buzz_cache_import(buzz_cache_t* cache, const void* k, const void* v, const f
 int buzz_cache_set_splits(buzz_cache_t* cache, int32_t n_splits);
 
 /*
- * Failure-handling aid.  The die-local merge (see BUZZ_FLAG_DEVICE_MERGE) checks in every decode step that
- * each block runs on the die the placement probe recorded for its launch-order number mod 8 (`die_map`:
- * 4 bits per number), and turns the attention output of a (batch, kv-head) pair whose blocks do not into NaN.
- * This call replaces the record the check compares with for one cache, so that a test can make the check
- * fail from the host (every kernel still runs to its end); a negative value restores the probe's record.
+ * Failure-handling aid.  The die-local merge (see BUZZ_FLAG_DEVICE_MERGE) checks in every decode step that the
+ * blocks of a (batch, kv-head) pair run on one die, whichever it is, and turns the pair's attention output into
+ * NaN where they do not.  With this call the steps of one cache also hold the die of each block against `die_map`
+ * (4 bits for each launch-order number mod 8), so that a test can make the check fail from the host (every kernel
+ * still runs to its end); a negative value takes that away again.
  * No effect where the die-local merge is not used.  Errors: BUZZ_EINVAL.
  */
 int buzz_cache_override_die_map(buzz_cache_t* cache, int64_t die_map);

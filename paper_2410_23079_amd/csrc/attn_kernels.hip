@@ -202,8 +202,10 @@ __device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 // units share), the same wait, the same ticket.  The hardware argument is the same with "the die's L2" in
 // place of "the memory side".  It lies outside the language memory model, which knows no scope between one
 // workgroup and the device, so it is guarded twice: the host enables it only on a GPU where a probe launch
-// has shown that block numbers equal mod 8 share a die, and every block compares the die it actually runs on
-// with the probe's record and flags a difference in the ticket, which turns the unit's output into NaN.
+// has shown that block numbers equal mod 8 share a die, and every block adds the die it actually runs on to the ticket,
+// in which the last one sees whether all were the same; if not, the unit's output is NaN.  Which die it is does not matter:
+// block 0 of a launch begins on die 0 on most hardware queues, on another on some of those that a process with several
+// streams gets.
 // BUZZ_FLAG_DEVICE_MERGE selects the device-wide form everywhere.
 template <bool LOCAL> constexpr int merge_scope() { return LOCAL ? __HIP_MEMORY_SCOPE_WORKGROUP : __HIP_MEMORY_SCOPE_AGENT; }
 template <bool LOCAL> __device__ inline void publish(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, merge_scope<LOCAL>()); }
@@ -690,31 +692,36 @@ __device__ inline void finish_split(const AttnArgs& a, const SplitCtx& x, SideRo
         __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0), expcnt / lgkmcnt untouched
         __syncthreads();
         if (tid == 0) {
-            // A die-local merge is only right if this block really runs where its number says: the host has
-            // recorded which die served block numbers 0..7 (die_map, 4 bits each); a block that finds itself
-            // elsewhere says so in the ticket's upper half, and the merging block sees every earlier arrival's.
+            // A die-local merge is only right if the unit's blocks share a die.  The ticket counts the arrivals (8 bits) and
+            // sums their dies (10 bits) and the dies' squares (13 bits): n blocks are on one die just where n times the sum
+            // of squares is the square of the sum.  A block that finds itself elsewhere than a record given with the step
+            // says (xcd_local 2) adds one to the squares, after which the two cannot be equal.
+            static_assert(kMaxSplits <= 128, "128 arrivals, 128 * 7 and 128 * (49 + 1) fit their fields");
             int add = 1, before;
             if (a.xcd_local) {
-                if ((__builtin_amdgcn_s_getreg((31 << 11) | 20) & 7u) != ((a.die_map >> (4 * x.home)) & 15u)) add += 0x10000;   // XCC_ID
+                const int die = (int)(__builtin_amdgcn_s_getreg((31 << 11) | 20) & 7u);   // XCC_ID
+                add += (die << 8) + ((die * die) << 18);
+                if (a.xcd_local == 2 && die != (int)((a.die_map >> (4 * x.home)) & 15u)) add += 1 << 18;
                 before = __hip_atomic_fetch_add(a.ticket + unit, add, __ATOMIC_RELAXED, merge_scope<true>());
             } else {
                 before = __hip_atomic_fetch_add(a.ticket + unit, add, __ATOMIC_RELAXED, merge_scope<false>());
             }
-            sm.ticket = before + (add & 0x10000);
+            sm.ticket = before + add;
         }
         __syncthreads();
         if (tid == 0) BUZZ_STAMP(4);
         const int arrival = __builtin_amdgcn_readfirstlane(sm.ticket);
-        if ((arrival & 0xffff) == S - 1) {
+        if ((arrival & 0xff) == S) {
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+            const int dies = (arrival >> 8) & 0x3ff;
             // merging threads: the lower half starts its side phase, unless the block has only 4 waves for a wide output, or a
             // short split's side phase and more groups of outputs than waves (2 units, 32 splits of 125 rows, 8 heads of 128: 10.1
             // us per step, 9.25 so; with 4 heads 8 units, 13 splits, half of them: 6.82, all 6.91)
             constexpr int NM = G * D >= kWideBlockMaxGD || (ONE_ROUND && G * D / 64 > NW) ? NTHR : NTHR / 2;
             if (tid >= NTHR - NM) {
-                // A die-local merge with a block on an unexpected die may have missed partials: its output is NaN
-                // rather than plausible numbers.
-                merge_splits<G, D, NM>(a, unit, __builtin_amdgcn_readfirstlane((tid - (NTHR - NM)) >> 6), (arrival >> 16) != 0, outp);
+                // A die-local merge of blocks on different dies may have missed partials: its output is NaN rather than
+                // plausible numbers.
+                merge_splits<G, D, NM>(a, unit, __builtin_amdgcn_readfirstlane((tid - (NTHR - NM)) >> 6), S * (arrival >> 18) != dies * dies, outp);
                 if (tid == NTHR - NM) {                   // ready for the next step
                     if (a.xcd_local) __hip_atomic_store(a.ticket + unit, 0, __ATOMIC_RELAXED, merge_scope<true>());
                     else __hip_atomic_store(a.ticket + unit, 0, __ATOMIC_RELAXED, merge_scope<false>());

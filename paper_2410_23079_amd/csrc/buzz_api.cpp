@@ -46,10 +46,9 @@ __global__ void die_probe_kernel(int32_t* out)
 }
 
 int g_die_local[kMaxDevices];          // per GPU: 0 not probed yet, 1 blocks b and b + 8 share a die, 2 they do not
-uint32_t g_die_map[kMaxDevices];       // per GPU: the die of block numbers 0..7, 4 bits each
 
 // The die-local merge of the decode kernel relies on the hardware dealing the blocks of a grid to the dies
-// round-robin in launch order (block b on die b mod 8), so that blocks whose numbers agree mod 8 share a die
+// round-robin in launch order (block b on die (b + r) mod 8, with an r of the hardware queue), so that blocks whose numbers agree mod 8 share a die
 // and its L2.  This checks that property once per GPU and process on two grid shapes, with one synchronisation
 // of `st`; where it does not hold the decode step merges through device memory as it does for other shapes.
 // Called from the prefill (never from a decode step, which must not synchronise).
@@ -71,20 +70,15 @@ int probe_die_placement(hipStream_t st)
     bool ok = true;
     for (int b = 8; b < kA; ++b) ok &= host[b] == host[b & 7];
     for (int b = 8; b < kB; ++b) ok &= host[kA + b] == host[kA + (b & 7)];
-    uint32_t map = 0;
-    for (int b = 0; b < 8; ++b) map |= (uint32_t)(host[b] & 7) << (4 * b);
-    g_die_map[dev] = map;
     g_die_local[dev] = ok ? 1 : 2;
     return BUZZ_OK;
 }
 
-// Whether this GPU passed the placement probe; *map = the die of block numbers 0..7.
-bool die_local_ok(uint32_t* map)
+// Whether this GPU passed the placement probe.
+bool die_local_ok()
 {
     int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices || g_die_local[dev] != 1) return false;
-    *map = g_die_map[dev];
-    return true;
+    return hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < kMaxDevices && g_die_local[dev] == 1;
 }
 
 constexpr uint32_t kMagic = 0xB0220C4Eu;
@@ -224,7 +218,7 @@ struct buzz_cache {
     int64_t sink_filled, n_old, tail, head, tokens_seen;
     int32_t user_splits;
     SplitModel split_model;
-    int64_t die_map_override;   // >= 0: use this instead of the placement probe's record (failure-handling tests)
+    int64_t die_map_override;   // >= 0: the record that the blocks' dies are held against (failure-handling tests)
     // the score update of the last decode step is applied lazily (by the next step or by a flush)
     bool pending;
     int last_buf;   // logit / stat buffer the last decode step wrote
@@ -843,9 +837,9 @@ int decode_step_impl(buzz_cache_t* c, const void* q, const void* k_new, const vo
         // a unit's splits on one die, merged through that die's L2: possible when the units divide evenly over
         // the 8 dies
         a.xcd_local = (a.n_splits > 1 && L.units % 8 == 0 && !(cfg.flags & BUZZ_FLAG_DEVICE_MERGE) &&
-                       die_local_ok(&a.die_map)) ? 1 : 0;
+                       die_local_ok()) ? 1 : 0;
         a.units_per_die = L.units / 8;
-        if (a.xcd_local && c->die_map_override >= 0) a.die_map = (uint32_t)c->die_map_override;
+        if (a.xcd_local && c->die_map_override >= 0) { a.xcd_local = 2; a.die_map = (uint32_t)c->die_map_override; }
         if (hipError_t e = launch_attn_split(cfg.kv_dtype, cfg.head_dim, L.G, a, L.units, st,
                                              static_scratch ? Timing{} : prof_pair(c, 0)))
             return hip_rc(e);

@@ -113,9 +113,9 @@ struct AttnArgs {
     int32_t s_cap;
     int32_t pending;     // 1: the previous step's score update has not been applied yet
     int32_t fixed_tiles; // 1: waves take tiles in a fixed round-robin (bitwise reproducible results)
-    int32_t xcd_local;   // 1: blocks are renumbered so that a unit's splits share one die, and merge through its L2
+    int32_t xcd_local;   // 1: blocks are renumbered so that a unit's splits share one die, and merge through its L2; 2: the same, die_map holds
     int32_t units_per_die;  // ... (the grid's z)
-    uint32_t die_map;    // ... and the die (4 bits each) that serves launch-order block numbers 0..7 mod 8
+    uint32_t die_map;    // 2: the die (4 bits each) that launch-order block numbers 0..7 mod 8 have to run on
     float scale_log2;    // softmax scale * log2(e)
     int32_t new_phys;    // physical row the appended token is written to
     int32_t new_pos;     // its original token index
