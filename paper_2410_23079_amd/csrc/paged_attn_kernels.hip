@@ -138,7 +138,10 @@ __device__ inline float2 acquire2(const float* p)
     const uint64_t v = __hip_atomic_load((const uint64_t*)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
 }
-constexpr int kParts = 16;                 // partial results that the merging block asks for at a time
+// Partial results that a team of the merging block asks for at a time, and teams.  The code that joins them runs once per launch
+// and is fetched while it runs, so more of either is slower: 8 pairs of 513 fp32 keys of 64 take 8.3 us with 16 and up to 16
+// teams, 8.2 with 8 and 16, 7.3 with 8 and 2 or 4; 32 pairs of 32768 keys in 8 bits 49.9, 49.9 and 49.6.
+constexpr int kParts = 8, kTeams = 2;
 
 // A block barrier that orders LDS alone: loads and stores to memory stay under way.
 __device__ inline void lds_barrier()
@@ -451,7 +454,7 @@ struct Sum2 { float ref, sum; float2 o; };             // of two output elements
 
 // A pair of which this block has only a part: publishes the part, and in the block that finishes last for the pair (for the
 // part's group first, where there are many) adds up all of them in order.  A thread takes two output elements; the heads are
-// laid over the threads as often as they fit, as teams that share the parts.  kParts parts are asked for at a time: one after
+// laid over the threads once or twice, as teams that share the parts.  kParts parts are asked for at a time: one after
 // the other, each would wait for memory.
 template <int D> __device__ inline void join_parts(const Parts& all, int slot, int64_t unit, const float2 (&stat)[NW][8], float (&acc)[NW][8][D], int* arrived)
 {
@@ -461,7 +464,7 @@ template <int D> __device__ inline void join_parts(const Parts& all, int slot, i
     const int tid = threadIdx.x, lane = tid & 63, j = lane % HL, G = a->G, e = tid % HT * 2;
     float* const part_o = a->part_o;
     float* const part_ml = a->part_ml;
-    const int padded = G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : 8, teams = padded < NH ? NH / padded : 1;
+    const int padded = G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : 8, teams = padded < NH ? min(NH / padded, kTeams) : 1;
     const int group = group_of(all.parts);
     bool last = group == 1;
     int first = last ? 0 : ((int)blockIdx.x - all.from) / group * group, stride = 1, count = last ? all.parts : min(group, all.parts - first), to = all.slot(first);
@@ -469,7 +472,7 @@ template <int D> __device__ inline void join_parts(const Parts& all, int slot, i
         for (int g0 = 0; g0 < G; g0 += NH) {
             const int g = g0 + (tid / HT & (padded < NH ? padded - 1 : NH - 1)), team = tid / HT / padded;
             Sum2 s{-3e38f, 0.f, make_float2(0.f, 0.f)};
-            if (g < G) {
+            if (g < G && team < teams) {
                 for (int p0 = team; p0 < count; p0 += kParts * teams) {
                     // lane j of a head's lanes fetches the (reference, sum) of its team's part p0 + j
                     auto at = [&](int k) { return (all.slot(first + min(p0 + k * teams, count - 1) * stride) * G + g); };
@@ -593,12 +596,13 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
             if (w.m < G) {
                 const int64_t row = (int64_t)pair * G + w.m;
                 const bool any = s.count > 0;
+                const float by = 1.f / w.sum;          // (a division for each output would be a fifth of the code that runs)
                 float* out = l->out + row * D + w.part * 4;
 #pragma unroll
                 for (int d = 0; d < D / 16; ++d) {
                     f32x4 x;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = any ? w.o[d][e] / w.sum : w.sum;   // nothing visible: 0, or NaN
+                    for (int e = 0; e < 4; ++e) x[e] = any ? w.o[d][e] * by : w.sum;   // nothing visible: 0, or NaN
                     *(f32x4*)(out + d * 16) = x;
                 }
                 if (w.part == 0 && l->lse) l->lse[row] = any ? (w.ref + log2f(w.sum)) * 0.6931471805599453f : w.sum - INFINITY;
