@@ -52,8 +52,7 @@ template <int P> struct Form {
                                                                           // their row's power of two, which f16 cannot hold
     // f16 weights are taken 2^8 times as large, so that what is lost below the type's range is 2^-32 of the largest one
     static constexpr float BIAS = F16V ? 8.f : 0.f;
-    // Tiles of a pair up to which one wave takes it: two, four where a tile costs little arithmetic; twice that where waves are
-    // hardly enough for the pairs.
+    // Tiles of a pair up to which one wave takes it: two, four where a tile costs little arithmetic.
     static constexpr int SOLO = EB == 2 ? 4 : 2;
 };
 constexpr float kSlack = 7.f;               // the reference moves when a logit exceeds it by 2^7: seldom after the first tiles
@@ -178,6 +177,7 @@ template <int P, int D, bool MASK> struct Attn {
     // ... and in 8 bits, whose elements are widened before each product, too few to have the next tile's keys under way behind
     // the values: both are asked for together (32 heads of 256, 4096 keys: 39.4 us with the keys first, 36.8 so).
     static constexpr bool LATE = D == 256 && F::E4M3;
+    static constexpr uint32_t MANY = D == 64 ? 5 : 4;  // pairs to two blocks that are many (below)
     struct Tile { int t0; int32_t pk, pv; };           // first key; pages of the keys that the lane loads of K, of V
 
     const PagedAttnArgs& a;
@@ -584,9 +584,13 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
     };
     A w(a, queries);
 
-    // Pairs of a few tiles: a wave to each, which needs nobody else.
-    const uint32_t pairs = (uint32_t)a.batch * H;
-    if (!A::QLDS && longest <= (pairs > 2 * a.blocks ? 2 : 1) * F::SOLO) {
+    // Pairs of a few tiles: a wave to each, which needs nobody else.  With two pairs and more to a block a few are three times as
+    // many for each of them, as far as pairs would be left whole: short pairs do not wait for long ones, and nothing is joined.
+    // (Heads of 64, whose tiles are half as much, from two and a half on: 16 sequences of 32 such heads with 600 8-bit keys take
+    // 12.2 us by blocks, 15 by waves; 20 sequences 18.4, 16.1.  64 sequences of 32 heads of 128 with 900 bf16 keys: 162 us by blocks, 156 by
+    // waves; of 90 to 900 keys 134 and 109; one of 900 and 63 of 90 118 and 37; 20 sequences of 500 35.4 and 33.0.)
+    const uint32_t pairs = (uint32_t)a.batch * H, whole = whole_tiles(F::TILE * D * F::EB * 2, pairs, a.blocks);
+    if (!A::QLDS && (uint32_t)longest <= (pairs < A::MANY * a.blocks / 2 ? (uint32_t)F::SOLO : min(whole, pairs / a.blocks * (3 * F::SOLO)))) {
         for (uint32_t pair = wave * a.blocks + blockIdx.x; pair < pairs; pair += a.blocks * NW) {   // over all compute units first
             const Segment s = segment(pair / H, pair % H);
             w.begin(s, 0, 1, wave);
@@ -621,7 +625,7 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(const PagedAttnArg
         for_lengths([&](int n) { sum += units_of(tiles_in(visible_in(n)).count, unit); });
         return sum;
     };
-    if ((uint32_t)longest <= whole_tiles(F::TILE * D * F::EB * 2, pairs, a.blocks)) unit = max(longest, 1);
+    if ((uint32_t)longest <= whole) unit = max(longest, 1);
     uint32_t mine = add(units_in_lane());
     if (per == 1 && 2 * pairs <= a.blocks && total > a.blocks) {
         unit *= units_per_block(total, a.blocks);
