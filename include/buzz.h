@@ -330,7 +330,8 @@ typedef struct buzz_rotary {
 /*
  * Norm and rotation of query and key rows, dense to dense: q [batch][n_q_heads][n_rows] to q_out, k likewise with
  * n_kv_heads to k_out.  Either pair may be NULL (both of it).  dtype BUZZ_FP32 / FP16 / BF16, head_dim 64, 128 or 256.
- * Errors: BUZZ_EINVAL, BUZZ_EUNSUPPORTED, BUZZ_EHIP.
+ * Errors: BUZZ_EINVAL, BUZZ_EUNSUPPORTED (other sizes, alignment, more than 65535 sequences or heads, 2^24 and more tiles
+ *         of 16 rows times heads), BUZZ_EHIP.
  */
 int buzz_qk_norm_rotate(int32_t dtype, int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const buzz_rotary_t* rotary,
                         const buzz_rows_t* q, const buzz_rows_t* k, const buzz_rows_t* q_out, const buzz_rows_t* k_out,
@@ -378,7 +379,11 @@ typedef struct buzz_pages {
     uint8_t* v_exp;
 } buzz_pages_t;
 
-/* Bytes of device workspace of a paged cache (partial results of buzz_paged_decode).  Errors: BUZZ_EINVAL, BUZZ_EUNSUPPORTED. */
+/*
+ * Bytes of device workspace of a paged cache (partial results of buzz_paged_decode).  Errors: BUZZ_EINVAL, BUZZ_EUNSUPPORTED
+ * (other sizes than those above, a page of 4 GiB, a sequence of more than 2^28 tokens, more than 65535 sequences or heads,
+ * 2^31 units of four tiles in all).
+ */
 int buzz_paged_workspace_bytes(const buzz_paged_config_t* cfg, size_t* bytes);
 
 /*
@@ -399,7 +404,7 @@ int buzz_paged_destroy(buzz_paged_t* cache);
  * token start[b] + t.  Queries, where given (q and q_out, both or neither), go through the same pass to q_out.  Tokens
  * beyond table_cols * page_rows are dropped.  No two rows of a call may go to the same row of a page.
  * Errors: BUZZ_EINVAL, BUZZ_ECAPACITY (batch above the configuration's, n_rows above table_cols * page_rows),
- *         BUZZ_EUNSUPPORTED (alignment), BUZZ_EHIP.
+ *         BUZZ_EUNSUPPORTED (alignment, too many rows times heads for one launch as above), BUZZ_EHIP.
  */
 int buzz_paged_append(buzz_paged_t* cache, const buzz_rotary_t* rotary, const buzz_rows_t* q, const buzz_rows_t* k,
                       const buzz_rows_t* v, const buzz_rows_t* q_out, int32_t batch, int64_t n_rows,

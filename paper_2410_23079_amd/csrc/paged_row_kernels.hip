@@ -341,9 +341,10 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const RotateArgs 
                     float ss = 0.f;
 #pragma unroll
                     for (int i = 0; i < N; ++i) ss = fmaf(x.x[i], x.x[i], ss);
-                    r = rsqrtf(row_sum<LPR>(ss) * (1.0f / D) + a.eps);
-#pragma unroll
-                    for (int i = 0; i < N; ++i) x.x[i] *= r;
+                    const float m = row_sum<LPR>(ss) * (1.0f / D) + a.eps;
+                    r = rsqrtf(m);
+                    const float off = fmaf(-m * r, r, 1.f);            // (its last bit is every element's: one step of Newton's)
+                    if (off < 1.f) r = fmaf(0.5f * r, off, r);         // (m 0, tiny or infinite: as it is)
                 }
 #pragma unroll
                 for (int i = 0; i < HN; ++i) {
@@ -351,8 +352,8 @@ __global__ __launch_bounds__(kThreads) void rotate_rows_kernel(const RotateArgs 
                     float& u2 = a.interleaved ? x.x[2 * i + 1] : x.x[HN + i];
                     const float v1 = u1, v2 = u2;
                     // (where nothing turns, the other element must not come in even with a weight of 0: it may be infinite)
-                    u1 = turns ? fmaf(v1, a1[i], -(v2 * b1[i])) : v1 * a1[i];
-                    u2 = turns ? fmaf(v2, a2[i], v1 * b2[i]) : v2 * a2[i];
+                    u1 = (turns ? fmaf(v1, a1[i], -(v2 * b1[i])) : v1 * a1[i]) * r;
+                    u2 = (turns ? fmaf(v2, a2[i], v1 * b2[i]) : v2 * a2[i]) * r;
                 }
                 if (E4M3 && to_page) {
                     const int e = exponent_for(row_max<LPR>(largest_finite<DT>(x)));

@@ -379,7 +379,9 @@ def test_decode_of_many_sequences(dtype, page_dtype):
 
 @pytest.mark.parametrize("B,H,G,D,dtype,page_dtype,longest,mask", [
     (70, 40, 1, 64, "bf16", None, 60, {}),                     # more pairs than waves, each a wave's; two lengths to a lane
-    (64, 8, 2, 128, "fp16", None, 480, {}),                    # whole pairs, two to a block
+    (64, 8, 2, 128, "fp16", None, 480, {}), (70, 8, 1, 128, "bf16", None, 768, {}),   # two to a block, a wave's up to 24 tiles
+    (70, 8, 1, 128, "bf16", None, 769, {}), (70, 8, 1, 128, "bf16", None, 1025, {}),  # whole for a block up to 32; cut
+    (70, 9, 2, 128, "fp16", "e4m3", 740, dict(sink=7, window=300)), (35, 60, 1, 64, "fp32", None, 700, {}),   # a wave's
     (40, 8, 1, 64, "bf16", "e4m3", 2500, {}),                  # blocks with parts of several pairs
     (33, 8, 3, 256, "bf16", None, 900, {}), (20, 8, 2, 128, "fp32", None, 1500, {}), (66, 4, 5, 256, "fp16", "e4m3", 400, {}),
     (48, 4, 8, 128, "fp16", "e4m3", 3000, dict(sink=100, window=1000)), (90, 3, 4, 128, "bf16", None, 1300, dict(sink=7, window=300)),
