@@ -17,12 +17,22 @@
 //     columns 8..15 (the same heads again) what that rounding left over, and in bf16 another product what is left then.
 //     The unused half of the matrix instruction does most of it for free.
 //
-// Layout of the work.  Sequences differ in length, and their lengths are known on the device only.  So the tiles of
-// all (sequence, head) pairs, 4 KG keys each, are numbered through, and each block takes the same number of
-// consecutive ones, whatever sequences they belong to: no block has more to do than another, and the grid does not
-// depend on how long a sequence may get.  A block's tiles of one pair are joined in LDS; a pair that lies within one
-// block is done, the others' partial results go through the workspace, and the block that finishes last for a pair
-// adds them up in order, which is why the result does not depend on timing.
+// Layout of the work.  Sequences differ in length, and their lengths are known on the device only.  So there is a block
+// of eight waves to every compute unit, and each looks at all lengths and finds its share by itself:
+//   - where pairs are short, or many and not long, a wave takes a whole pair and nothing is joined;
+//   - otherwise the tiles of all (sequence, head) pairs, 4 KG keys each, are cut into units of four tiles or more (a whole
+//     pair, where the longest is short; as much as gives every block one, where pairs are few), numbered through, and
+//     each block takes the same number of consecutive ones, whatever sequences they belong to: no block has more to do
+//     than another, and the grid does not depend on how long a sequence may get.  A block's tiles of one pair go to its
+//     waves in turn and are joined in LDS; a pair that lies within one block is done, the others' partial results go
+//     through the workspace, and the block that finishes last for a pair adds them up in order, which is why the result
+//     does not depend on timing.  The next pair's first rows are under way meanwhile.
+//
+// Measured (a call in a captured graph): 16 sequences of 32 bf16 heads of 128, up to 16384 keys, 378 us, 6.34 TB/s of the
+// 7.05 that a plain read reaches; 8 sequences of 32 fp16 heads, up to 4096, 57 us, 5.5 TB/s; 4 sequences of 8 pairs with 4
+// heads, 32768 keys in 8 bits, 50 us, 5.4 TB/s; 8 pairs with 4 heads of 1517 bf16 keys 9.3 us, of 300 8.3, of one 3.9.  Of 9
+// us: start 0.4 to 0.9 us, lengths 0.4, shares 0.6, page numbers 0.35, keys and
+// values 1.3 to 1.7, LDS 0.7, publish and ticket 1.0, the parts back 1.0, output 0.7.
 #include <math.h>
 
 #include "paged_internal.h"

@@ -11,6 +11,11 @@
 //     the dwords of 16 positions meet in LDS and leave as whole 16-byte pieces where all g rows of one are new, as single
 //     elements where they are not.  Tiles are aligned to 16 positions of the sequence, so that a piece and a page belong
 //     to one block, and its page is one number.
+// Measured (a call in a captured graph): 32768 tokens of 32 + 8 bf16 heads of 128 turned 137 us, 4.9 TB/s read and written, of
+// which a copy of these bytes takes 123; up to 8192 tokens of four sequences, the same heads into 8-bit pages, 107, and back 28;
+// 131072 tokens of 8 heads out of 8-bit pages 150 us, 5.4 TB/s; one token of 8 sequences 4.0 us.
+// 32 bits up to the rounding to 8: of 33 million codes some 38 are a neighbour of the exact value's.  In 64 bits it is 11, but
+// a SIMD then holds two waves instead of four and the call takes 20% longer.
 #include <math.h>
 
 #include "paged_internal.h"
